@@ -357,6 +357,127 @@ int64_t kv_cache_tokens(const kv_cache_t *cache);
 
 const char *kv_strerror(int code);
 
+/* ---- 4-bit paged cache ------------------------------------------------------
+ * A second cache beside the packed one, for batches whose sequences differ: every
+ * sequence has its own length and its own number of new tokens, attention takes
+ * one or many query rows of each, with an optional window.  Rows are held at a
+ * fixed rate in pages of KV_FP4_PAGE_TOKENS tokens that the caller hands out.
+ *
+ * Values (the block format of OCP Microscaling, MXFP4, with blocks along the head
+ * dimension): for every KV_FP4_GROUP consecutive channels x of a token and kv-head
+ * one scale 2^e, e the least integer with max|x| <= 7 * 2^e, kept within -23 .. 13;
+ * for every channel the sign and the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 to
+ * |x| / 2^e (ties to the even code, above 6: 6).  The value read is code * 2^e: it
+ * is exact in fp16, bf16 and fp32.  |x - value| <= 2^e where |x| <= 7 * 2^13 (half a
+ * step of the largest codes), magnitudes above 49152 and infinities are held as 49152
+ * with their sign, a NaN as 0: a cache holds finite values only.
+ *
+ * Layout of a page: n_kv_heads blocks of kv_fp4_head_bytes = 64 * (D + D / 16) bytes
+ * (D = head_dim):
+ *     K codes   byte [token][D / 2]: channel 2i in the low half of byte i, 2i + 1 in the high half
+ *     K scales  byte [token][D / 32]: e + 127
+ *     V codes   uint32 [token / 8][D]: bits 4i .. 4i + 3 hold token 8 * (token / 8) + i
+ *     V scales  byte [D / 32][token]: e + 127
+ * A code is sign << 3 | index into the magnitudes above.
+ *
+ * Which tokens a call is about is said by a kv_fp4_batch_t.  Its arrays are read on
+ * the device when the call's kernels run, so a captured call follows what they then
+ * hold.  Nothing they hold makes a kernel touch memory outside the page table, the pages
+ * and the rows: a page number outside 0 .. n_pages - 1 marks a page that is missing
+ * (its tokens are skipped by an append, read as zeros and seen by no row), and so are
+ * positions from 64 * table_pages on.
+ */
+#define KV_FP4_PAGE_TOKENS 64
+#define KV_FP4_GROUP 32
+
+typedef struct kv_fp4_cache kv_fp4_cache_t; /* opaque, host memory owned by the library */
+
+/* Types of rows that go in and come out. */
+#define KV_TYPE_FP16 0
+#define KV_TYPE_BF16 1
+#define KV_TYPE_FP32 2 /* outputs only */
+
+typedef struct {
+    int32_t n_kv_heads; /* H_kv >= 1                                              */
+    int32_t n_q_heads;  /* H_q, any multiple of H_kv                              */
+    int32_t head_dim;   /* 128 or 64                                              */
+    int64_t n_pages;    /* 1 .. 2^31 - 1                                          */
+} kv_fp4_config_t;
+
+/* Bytes of the two device buffers of a cache. */
+typedef struct {
+    size_t pages;     /* n_pages * n_kv_heads * 64 * (head_dim + head_dim / 16)   */
+    size_t workspace; /* partial results of attention                             */
+} kv_fp4_sizes_t;
+
+/* A ragged batch: sequence b holds lens[b] tokens, the last new_rows[b] of which
+ * are the call's; row i of them lies at row first_row[b] + i of the call's tensors
+ * and at position lens[b] - new_rows[b] + i of the sequence.  All arrays are device
+ * memory.  Rows outside the tensors are left out. */
+typedef struct {
+    int32_t batch;             /* sequences >= 1                                  */
+    int32_t max_new;           /* most new rows of a sequence; new_rows above it count as it */
+    int32_t table_pages;       /* pages of a sequence at most: 1 .. 2^24          */
+    const int32_t *lens;       /* [batch], negative: 0                            */
+    const int32_t *new_rows;   /* [batch]; null: max_new of every sequence        */
+    const int32_t *first_row;  /* [batch]; null: b * max_new                      */
+    const int32_t *page_table; /* [batch][table_pages]; null: page i of sequence b is b * table_pages + i */
+} kv_fp4_batch_t;
+
+/* Host only. */
+int kv_fp4_query_sizes(const kv_fp4_config_t *cfg, kv_fp4_sizes_t *out);
+/*
+ * A cache over caller-owned device buffers, both 256-byte aligned and at least as
+ * large as kv_fp4_query_sizes said; valid until kv_fp4_cache_destroy.  Host
+ * bookkeeping only: the pages' contents are taken as they are (pages that another
+ * cache of the same configuration has filled can be used).
+ */
+int kv_fp4_cache_create(const kv_fp4_config_t *cfg, void *pages, void *workspace, const kv_fp4_sizes_t *sizes,
+                        kv_fp4_cache_t **out);
+int kv_fp4_cache_destroy(kv_fp4_cache_t *cache);
+
+/*
+ * Quantizes the batch's new rows and writes them into their pages.  k, v: device
+ * [n_rows][H_kv][D] of `type` (KV_TYPE_FP16 or KV_TYPE_BF16), consecutive rows k_stride
+ * and v_stride elements apart (at least H_kv * D; multiples of 8, pointers 16-byte
+ * aligned: k and v may be parts of one projection's output).  Other tokens of the pages
+ * keep their values.  A page that is written must belong to one sequence of
+ * the call only; full pages may be shared by sequences.
+ */
+int kv_fp4_append(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, const void *k, int64_t k_stride, const void *v,
+                  int64_t v_stride, int32_t type, int64_t n_rows, void *hip_stream);
+/*
+ * The values of the batch's new rows as the cache holds them (new_rows = lens: of
+ * whole sequences).  k, v: device [n_rows][H_kv][D], contiguous, 16-byte aligned, of
+ * `type` (any of the three: the values are exact in each); one of them may be null.
+ * Rows of no sequence are left as they were; a row whose position the sequence does not
+ * have (new_rows above lens) or whose page is missing is zeros.
+ */
+int kv_fp4_read(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, void *k, void *v, int32_t type, int64_t n_rows,
+                void *hip_stream);
+/*
+ * Attention of the batch's new rows over their sequences (append them first):
+ *   out[row][hq][:] = sum_t softmax_t(sm_scale * q[row][hq] . Khat[t][hq / G]) * Vhat[t][hq / G][:]
+ * over the tokens t that the row at position p sees: t <= p, and with window > 0 also
+ * t > p - window or t < sinks (the first tokens stay visible).  window = 0: no
+ * window.  Tokens that no row sees are not read: their pages may be missing.  A row that
+ * sees nothing becomes zeros (lse: -infinity).
+ * q: device [n_rows][H_q][D] of `type` (fp16 or bf16), rows q_stride elements apart (a
+ * multiple of 8, at least H_q * D), 16-byte aligned; out: device [n_rows][H_q][D]
+ * contiguous of `out_type` (any), 16-byte aligned; lse: null, or device fp32
+ * [n_rows][H_q], the natural logarithm of the softmax's sum (with the scores' maximum
+ * in it), for joining this result with one over other tokens.  Rows of no sequence are
+ * left as they were.
+ * q.Khat: exact products on the matrix cores, fp32 sums; softmax in fp32; its weights
+ * enter the product with Vhat as fp16 (scaled by a power of two: a relative error of
+ * at most 2^-11 down to 2^-29 of the row's largest weight), sums in fp32.  A NaN or
+ * infinity in q stays with its row and head.  Sums have a fixed order: the result
+ * is bitwise reproducible.  Uses the workspace: attention calls on one cache must not overlap.
+ */
+int kv_fp4_attention(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, const void *q, int64_t q_stride, int32_t type,
+                     int64_t n_rows, float sm_scale, int32_t window, int32_t sinks, void *out, int32_t out_type,
+                     float *lse, void *hip_stream);
+
 /* ---- measurement companions (same shapes, uncompressed fp16 cache) ---------
  * The comparison kernels of Sec. IV-E, hand-written for the same shapes:
  * plain fp16 matrix-vector products over an uncompressed cache stored as

@@ -56,11 +56,30 @@ class kv_stats_t(C.Structure):
                 ("v_header_bytes", C.c_int64), ("v_payload_bytes", C.c_int64), ("v_padding_bytes", C.c_int64)]
 
 
+FP4_PAGE_TOKENS, FP4_GROUP = 64, 32
+KV_TYPE_FP16, KV_TYPE_BF16, KV_TYPE_FP32 = 0, 1, 2
+
+
+class kv_fp4_config_t(C.Structure):
+    _fields_ = [("n_kv_heads", C.c_int32), ("n_q_heads", C.c_int32), ("head_dim", C.c_int32), ("n_pages", C.c_int64)]
+
+
+class kv_fp4_sizes_t(C.Structure):
+    _fields_ = [("pages", C.c_size_t), ("workspace", C.c_size_t)]
+
+
+class kv_fp4_batch_t(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("max_new", C.c_int32), ("table_pages", C.c_int32),
+                ("lens", C.c_void_p), ("new_rows", C.c_void_p), ("first_row", C.c_void_p), ("page_table", C.c_void_p)]
+
+
 EXPORTS = ("kv_query_sizes", "kv_cache_create", "kv_cache_destroy", "kv_compress_append", "kv_compress_append_bf16",
            "kv_k_matvec", "kv_v_matvec", "kv_v_matvec_noalloc", "kv_softmax", "kv_decode_attention", "kv_cache_stats", "kv_cache_restore", "kv_cache_tokens",
            "kv_strerror", "kv_fp16_k_matvec", "kv_fp16_v_matvec", "kv_fp16_v_workspace_bytes",
            "kv_stream_read", "kv_page_pool_state_bytes", "kv_page_pool_create", "kv_page_pool_destroy",
-           "kv_page_pool_free_pages", "kv_query_sizes_paged", "kv_cache_create_paged", "kv_cache_release")
+           "kv_page_pool_free_pages", "kv_query_sizes_paged", "kv_cache_create_paged", "kv_cache_release",
+           "kv_fp4_query_sizes", "kv_fp4_cache_create", "kv_fp4_cache_destroy", "kv_fp4_append", "kv_fp4_read",
+           "kv_fp4_attention")
 # entry points the native module calls, in its order
 _NATIVE_CALLS = ("kv_compress_append", "kv_compress_append_bf16", "kv_k_matvec", "kv_softmax", "kv_v_matvec",
                  "kv_decode_attention", "kv_cache_restore", "kv_cache_release", "kv_cache_tokens")
@@ -141,6 +160,13 @@ def lib():
         L.kv_fp16_v_workspace_bytes.argtypes = [i32, i32]
         L.kv_fp16_v_workspace_bytes.restype = C.c_size_t
         L.kv_stream_read.argtypes = [vp, C.c_size_t, vp, vp]
+        batch = C.POINTER(kv_fp4_batch_t)
+        L.kv_fp4_query_sizes.argtypes = [C.POINTER(kv_fp4_config_t), C.POINTER(kv_fp4_sizes_t)]
+        L.kv_fp4_cache_create.argtypes = [C.POINTER(kv_fp4_config_t), vp, vp, C.POINTER(kv_fp4_sizes_t), C.POINTER(vp)]
+        L.kv_fp4_cache_destroy.argtypes = [vp]
+        L.kv_fp4_append.argtypes = [vp, batch, vp, i64, vp, i64, i32, i64, vp]
+        L.kv_fp4_read.argtypes = [vp, batch, vp, vp, i32, i64, vp]
+        L.kv_fp4_attention.argtypes = [vp, batch, vp, i64, i32, i64, f32, i32, i32, vp, i32, vp, vp]
         for name in EXPORTS:
             if name not in ("kv_cache_tokens", "kv_strerror", "kv_fp16_v_workspace_bytes",
                             "kv_page_pool_state_bytes"):
@@ -405,6 +431,154 @@ class PackedKVCache:
     # typed views of the raw buffers, for tests and tools
     def view(self, name, dtype):
         return self.tensors[name].view(dtype)
+
+
+_TYPES = {torch.float16: KV_TYPE_FP16, torch.bfloat16: KV_TYPE_BF16, torch.float32: KV_TYPE_FP32}
+
+
+def _refuse(what, why):
+    raise PackKVError("%s: %s" % (what, why), KV_ERR_ARG)
+
+
+class FP4Batch:
+    """What a call on an FP4KVCache is about (kv_fp4_batch_t): sequence b holds lens[b] tokens, the last new_rows[b] of which
+    are rows first_row[b], first_row[b] + 1, ... of the call's tensors.  lens, new_rows, first_row: int32 device tensors
+    [batch]; page_table: int32 [batch, pages of a sequence at most].  Without new_rows every sequence has max_new of them, without first_row
+    sequence b's begin at row b * max_new, without page_table sequence b has pages b * table_pages .. of the cache.
+    The tensors are kept and read when a call's kernels run: a program changes their contents from step to step."""
+
+    def __init__(self, lens, max_new, page_table=None, new_rows=None, first_row=None, table_pages=None):
+        what = "FP4Batch"
+        if lens.dim() != 1 or lens.shape[0] < 1:
+            _refuse(what, "lens is [batch]")
+        self.batch, self.max_new, self.device = lens.shape[0], int(max_new), lens.device
+        for name, t in (("lens", lens), ("new_rows", new_rows), ("first_row", first_row)):
+            if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != (self.batch,) or not t.is_contiguous()):
+                _refuse(what, "%s is int32 [batch], contiguous" % name)
+        if page_table is not None:
+            if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.shape[0] != self.batch or \
+                    not page_table.is_contiguous() or table_pages not in (None, page_table.shape[1]):
+                _refuse(what, "page_table is int32 [batch, table_pages], contiguous")
+            table_pages = page_table.shape[1]
+        elif table_pages is None:
+            _refuse(what, "page_table or table_pages")
+        if any(t is not None and t.device != self.device for t in (new_rows, first_row, page_table)):
+            _refuse(what, "tensors of one device")
+        self.table_pages = int(table_pages)
+        if not (0 <= self.max_new < 2 ** 31 and 1 <= self.table_pages < 2 ** 31):
+            _refuse(what, "max_new is 0 or more, table_pages 1 or more")
+        self.lens, self.new_rows, self.first_row, self.page_table = lens, new_rows, first_row, page_table
+        self._c = kv_fp4_batch_t(self.batch, self.max_new, self.table_pages,
+                                 *(None if t is None else t.data_ptr() for t in (lens, new_rows, first_row, page_table)))
+        self._ref = C.byref(self._c)
+
+
+class FP4KVCache:
+    """A 4-bit paged cache (packkv.h: MXFP4 rows in pages of 64 tokens): owns the pages and the workspace (torch tensors)
+    and the kv_fp4_cache_t handle.  Which pages a sequence has, and how long it is, is the program's (FP4Batch)."""
+
+    def __init__(self, n_pages, n_kv_heads, n_q_heads, head_dim=HEAD_DIM, device="cuda:0"):
+        self.cfg = kv_fp4_config_t(n_kv_heads, n_q_heads, head_dim, n_pages)
+        self.device = torch.device(device)
+        sizes = kv_fp4_sizes_t()
+        _check(lib().kv_fp4_query_sizes(C.byref(self.cfg), C.byref(sizes)), "kv_fp4_query_sizes")
+        self.pages = torch.empty(sizes.pages, dtype=torch.uint8, device=self.device)
+        self.workspace = torch.empty(sizes.workspace, dtype=torch.uint8, device=self.device)
+        self.device = self.pages.device
+        handle = C.c_void_p()
+        _check(lib().kv_fp4_cache_create(C.byref(self.cfg), self.pages.data_ptr(), self.workspace.data_ptr(),
+                                         C.byref(sizes), C.byref(handle)), "kv_fp4_cache_create")
+        self.handle = handle
+        self.n_pages, self.n_kv_heads, self.n_q_heads, self.head_dim = n_pages, n_kv_heads, n_q_heads, head_dim
+
+    def close(self):
+        if getattr(self, "handle", None) and _lib is not None:
+            _lib.kv_fp4_cache_destroy(self.handle)
+        self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _rows(self, what, t, heads, types):
+        """Rows and row stride of t: [rows, heads, D] or [batch, n, heads, D], the heads of a row next to each other."""
+        if t.device != self.device or t.dtype not in types:
+            _refuse(what, "tensors of %s on %s" % (" or ".join(map(str, types)), self.device))
+        shape, stride = t.shape, t.stride()
+        if t.dim() not in (3, 4) or shape[-2:] != (heads, self.head_dim) or \
+                stride[-1] != 1 or (heads > 1 and stride[-2] != self.head_dim):
+            _refuse(what, "[rows, %d, %d], the heads of a row next to each other" % (heads, self.head_dim))
+        if t.dim() == 3:
+            rows, pitch = shape[0], stride[0]
+        else:
+            rows, pitch = shape[0] * shape[1], stride[1] if shape[1] > 1 else stride[0]
+            if shape[0] > 1 and shape[1] > 1 and stride[0] != shape[1] * stride[1]:
+                _refuse(what, "rows at even distances")
+        return rows, pitch if rows > 1 else heads * self.head_dim
+
+    def _call(self, what, function, batch, stream, *args):
+        if not self.handle:
+            _refuse(what, "the cache is closed")
+        if batch.device != self.device:
+            _refuse(what, "the batch is on %s, the cache on %s" % (batch.device, self.device))
+        if _current_device is not None and _current_device() == self.device.index:
+            rc = function(self.handle, batch._ref, *args, _stream_ptr(stream))
+        else:
+            with torch.cuda.device(self.device):
+                rc = function(self.handle, batch._ref, *args, _stream_ptr(stream))
+        if rc != KV_OK:
+            _check(rc, what)
+
+    def _used_on(self, stream, *tensors):
+        """Tensors made here are used on `stream`, which need not be the one they were made on."""
+        if stream is not None:
+            on = torch.cuda.ExternalStream(stream, device=self.device) if isinstance(stream, int) else stream
+            for t in tensors:
+                t.record_stream(on)
+
+    def kv_fp4_append(self, k, v, batch, stream=None):
+        """k, v: fp16 or bf16 [rows, H_kv, D] (or [batch, n, H_kv, D]); may be parts of wider rows."""
+        half = (torch.float16, torch.bfloat16)
+        rows, k_stride = self._rows("kv_fp4_append", k, self.n_kv_heads, half)
+        v_rows, v_stride = self._rows("kv_fp4_append", v, self.n_kv_heads, half)
+        if rows != v_rows or k.dtype != v.dtype:
+            _refuse("kv_fp4_append", "k and v of as many rows and of one type")
+        self._call("kv_fp4_append", _lib.kv_fp4_append, batch, stream, k.data_ptr(), k_stride, v.data_ptr(), v_stride,
+                   _TYPES[k.dtype], rows)
+
+    def kv_fp4_read(self, batch, n_rows, dtype=torch.float16, k=None, v=None, stream=None):
+        """The batch's new rows as the cache holds them: (k, v), [n_rows, H_kv, D] of dtype; rows of no sequence are not written."""
+        what, shape = "kv_fp4_read", (n_rows, self.n_kv_heads, self.head_dim)
+        if dtype not in _TYPES:
+            _refuse(what, "dtype is float16, bfloat16 or float32")
+        made = [torch.empty(shape, dtype=dtype, device=self.device) if t is None else t for t in (k, v)]
+        for t in made:
+            if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != self.device:
+                _refuse(what, "k and v are contiguous %s %s on %s" % (shape, dtype, self.device))
+        self._call(what, _lib.kv_fp4_read, batch, stream, made[0].data_ptr(), made[1].data_ptr(), _TYPES[dtype], n_rows)
+        self._used_on(stream, *made)
+        return tuple(made)
+
+    def kv_fp4_attention(self, q, batch, sm_scale, window=0, sinks=0, out=None, lse=None, stream=None):
+        """q: fp16 or bf16 [rows, H_q, D] (or [batch, n, H_q, D]) -> out [rows, H_q, D] of q's type (or of out's: fp16, bf16,
+        fp32); lse: fp32 [rows, H_q] that gets the logarithms of the softmax sums.  Rows of no sequence are not written."""
+        what = "kv_fp4_attention"
+        rows, q_stride = self._rows(what, q, self.n_q_heads, (torch.float16, torch.bfloat16))
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
+        elif out.dtype not in _TYPES or out.shape != q.shape or not out.is_contiguous() or out.device != self.device:
+            _refuse(what, "out is contiguous, of q's shape and on its device")
+        if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:-1] or not lse.is_contiguous() or
+                                lse.device != self.device):
+            _refuse(what, "lse is contiguous fp32, of q's shape without the last axis")
+        if not (0 <= window < 2 ** 31 and 0 <= sinks < 2 ** 31):
+            _refuse(what, "window and sinks are 0 or more")
+        self._call(what, _lib.kv_fp4_attention, batch, stream, q.data_ptr(), q_stride, _TYPES[q.dtype], rows, sm_scale,
+                   window, sinks, out.data_ptr(), _TYPES[out.dtype], None if lse is None else lse.data_ptr())
+        self._used_on(stream, out)
+        return out
 
 
 def kv_fp16_k_matvec(k_cache, q, sm_scale, n_kv_heads, scores=None, stream=None):

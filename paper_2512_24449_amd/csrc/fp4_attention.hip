@@ -1,0 +1,369 @@
+// Attention over the 4-bit paged cache, one pass with the running maximum and sum of a softmax.
+//
+// Scores are computed transposed: S^T = K Q^T (rows: tokens, columns: the query heads of a kv-head, of one or several new
+// rows), then O^T = V^T P^T.  A lane then holds scores, weights and outputs of one column only, so maximum and sum are the
+// lane's own (joined over the four lanes of a column), and the layout in which the matrix cores leave S^T is the one in which
+// they take P^T: nothing passes through LDS or other lanes between the two products.  Which 32 tokens a step's rows stand
+// for is free as long as both products agree; row 4g + i of the first (second) product of 16 is token 8g + i (8g + 4 + i), so
+// that a lane's eight weights are eight consecutive tokens: a word of V.
+//
+// K and V enter as fp16 (K as bf16 where q is): E2M1 numbers with scales 2^-23 .. 2^13 are exact there.
+#include <algorithm>
+
+#include "fp4.h"
+#include "unpack.h"
+
+namespace packkv {
+
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf162_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf168_t __attribute__((ext_vector_type(8)));
+typedef float float4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
+
+constexpr int FP4_STEP = 32;             // tokens of a step: half a page
+constexpr int FP4_COLUMNS = 16;
+// Weights are held as 2^P_LIFT times their size: the largest is then 2^15, and fp16 keeps its eleven bits down to 2^-29.
+constexpr float P_LIFT = 15.0f;
+// Partial results: at most so many rows (of a column in a split) of HD + 4 floats.
+constexpr int64_t FP4_PART_ROWS = 32768;
+constexpr int FP4_SPLITS_MAX = 256;
+
+size_t fp4_workspace_bytes(int head_dim) { return size_t(FP4_PART_ROWS) * (head_dim + 4) * sizeof(float); }
+
+struct Fp4Attention {
+    Fp4View v;
+    const uint16_t *q;
+    int64_t q_stride;
+    float scale;             // sm_scale * log2(e)
+    int window, sinks;
+    void *out;
+    int out_type;
+    float *lse;
+    float *part;             // [(column block, kv-head, sequence)][split][column]: HD sums, maximum, sum; null: one split
+    int splits, blocks;      // splits of the context, column blocks
+};
+
+// Four words of a row (32 values' codes, HD / 4 of a lane) as operands: value pairs in the order of the channels.
+template <bool BF16>
+__device__ inline uint4_t row_operand(uint32_t w, float scale) {
+    if constexpr (BF16)
+        return uint4_t{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
+                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
+                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)),
+                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3))};
+    else
+        return uint4_t{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0)),
+                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1)),
+                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2)),
+                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3))};
+}
+
+template <bool BF16>
+__device__ inline float4_t product16(uint4_t a, uint4_t b, float4_t c) {
+    if constexpr (BF16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf168_t, a), __builtin_bit_cast(bf168_t, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
+}
+
+// The scales of eight tokens (bytes e + 127) as fp16 pairs.
+__device__ inline void scale_pairs(uint2 bytes, half2_t (&out)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t two = (i < 2 ? bytes.x : bytes.y) >> (16 * (i & 1));
+        out[i] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_pkrtz(__uint_as_float((two & 255u) << 23),
+                                                                         __uint_as_float(((two >> 8) & 255u) << 23)));
+    }
+}
+
+// A word of V (one channel of eight tokens) with the tokens' scales.
+__device__ inline uint4_t column_operand(uint32_t w, const half2_t (&scale)[4]) {
+    uint4_t r;
+    r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 0) * scale[0]);
+    r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 1) * scale[1]);
+    r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 2) * scale[2]);
+    r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 3) * scale[3]);
+    return r;
+}
+
+// Sum or maximum over the four lanes of a column (lane, lane ^ 16, lane ^ 32, lane ^ 48).
+__device__ inline float column_max(float x) {
+    x = fmaxf(x, __shfl_xor(x, 16));
+    return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ inline float column_sum(float x) {
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+}
+
+// exp2(a - b) where -inf - -inf means no weight.
+__device__ inline float weight_of(float a, float b) { return b == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(a - b); }
+
+template <int N>
+__device__ inline void store_out(void *out, int type, int64_t at, const float (&x)[N]) {
+    if (type == KV_TYPE_FP32) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4)
+            *reinterpret_cast<float4 *>(static_cast<float *>(out) + at + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+        return;
+    }
+    uint32_t w[N / 2];
+#pragma unroll
+    for (int i = 0; i < N; i += 2)
+        w[i / 2] = type == KV_TYPE_BF16 ? __builtin_bit_cast(uint32_t, bf162_t{__bf16(x[i]), __bf16(x[i + 1])})
+                                        : __builtin_bit_cast(uint32_t, half2_t{_Float16(x[i]), _Float16(x[i + 1])});
+#pragma unroll
+    for (int i = 0; i < N / 2; i += 2)
+        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(out) + at + 2 * i) = make_uint2(w[i], w[i + 1]);
+}
+
+// The tokens that a block of columns sees, in steps of 32: those that hold first tokens, then those from the window's
+// start to the last row.
+struct Fp4Steps {
+    int first_row, last_row;   // new rows of the block
+    int end;                   // tokens from here on are seen by none
+    int begin;                 // nor are those below, but for the first ones
+    int sink_steps, window_step, n;
+    __device__ inline Fp4Steps(const Fp4Sequence &seq, int column0, int columns, int G, int window, int sinks) {
+        first_row = column0 / G;
+        last_row = min((column0 + columns - 1) / G, seq.n - 1);
+        end = min(seq.pos0 + last_row + 1, seq.held);
+        begin = window ? max(max(seq.pos0 + first_row, 0) - window + 1, 0) : 0;
+        window_step = begin / FP4_STEP;
+        sink_steps = min((min(window ? sinks : 0, max(end, 0)) + FP4_STEP - 1) / FP4_STEP, window_step);
+        n = end > 0 ? sink_steps + max((end + FP4_STEP - 1) / FP4_STEP - window_step, 0) : 0;
+    }
+    __device__ inline int token(int step) const { return FP4_STEP * (step < sink_steps ? step : step - sink_steps + window_step); }
+};
+
+template <int HD, bool BF16>
+__global__ __launch_bounds__(256) void fp4_attention_kernel(Fp4Attention a) {
+    using P = Fp4Block<HD>;
+    constexpr int KW = HD / 32;          // words of K in a lane's quarter of a row; products of 32 channels
+    constexpr int VH = HD / 64;          // 16-byte pieces of V per lane
+    constexpr int OT = HD / 16;          // blocks of 16 channels
+    __shared__ float lds_o[4][FP4_COLUMNS][HD + 4];
+    __shared__ float lds_m[4][FP4_COLUMNS], lds_l[4][FP4_COLUMNS];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c16 = lane & 15, g = lane >> 4;
+    const Fp4View &v = a.v;
+    const int split = int(blockIdx.x % a.splits);
+    const int64_t rest = blockIdx.x / a.splits;
+    const int h = int(rest % v.H), b = int(rest / v.H % v.batch.batch), block = int(rest / v.H / v.batch.batch);
+    const Fp4Sequence seq(v, b);
+    const int column0 = block * FP4_COLUMNS, columns = seq.n * v.G;
+    if (column0 >= columns) return;
+    const Fp4Steps steps(seq, column0, FP4_COLUMNS, v.G, a.window, a.sinks);
+    const int per_split = (steps.n + a.splits - 1) / a.splits;
+    const int step_end = min((split + 1) * per_split, steps.n);
+
+    // this lane's column
+    const int column = column0 + c16, row = column / v.G, head = h * v.G + column % v.G;
+    const int64_t out_row = seq.first + row;
+    const bool real = column < columns && out_row >= 0 && out_row < v.n_rows;
+    const int hi = max(seq.pos0 + row, -1), lo = a.window ? hi - a.window + 1 : 0;
+    uint4_t q[KW];
+#pragma unroll
+    for (int i = 0; i < KW; ++i) {
+        q[i] = uint4_t{0, 0, 0, 0};
+        if (real) q[i] = *reinterpret_cast<const uint4_t *>(a.q + out_row * a.q_stride + int64_t(head) * HD + g * (HD / 4) + 8 * i);
+    }
+
+    float4_t o[OT];
+#pragma unroll
+    for (int i = 0; i < OT; ++i) o[i] = float4_t{0, 0, 0, 0};
+    float m = -INFINITY, l = 0.0f;
+
+    for (int step = split * per_split + wave; step < step_end; step += 4) {
+        const int t0 = steps.token(step);
+        const int64_t page = seq.page(v, t0 / FP4_PAGE);
+        if (page < 0) continue;
+        const uint8_t *data = v.pages + (page * v.H + h) * size_t(P::BYTES);
+        const int at = t0 % FP4_PAGE;
+        // scores of tokens t0 + 8g + 4t + i, i < 4, in s[t]
+        float s[8];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int token = at + 8 * (c16 >> 2) + 4 * t + (c16 & 3);
+            uint32_t w[KW];
+            const uint8_t *from = data + P::K + token * (HD / 2) + g * (HD / 8);
+            if constexpr (KW == 4) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(from);
+                w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+            } else {
+                const uint2 x = *reinterpret_cast<const uint2 *>(from);
+                w[0] = x.x, w[1] = x.y;
+            }
+            const float scale = __uint_as_float(uint32_t(data[P::KS + token * (HD / FP4_GROUP) + g * (HD / 4) / FP4_GROUP]) << 23);
+            float4_t acc = {0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < KW; ++i) acc = product16<BF16>(row_operand<BF16>(w[i], scale), q[i], acc);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[4 * t + i] = acc[i] * a.scale;
+        }
+        const int t8 = t0 + 8 * g;
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int t = t8 + i;
+            if (!(t <= hi && t < steps.end && (t >= lo || t < a.sinks))) s[i] = -INFINITY;
+            top = fmaxf(top, s[i]);
+        }
+        top = column_max(top);
+        if (top > m) {
+            const float f = weight_of(m, top);
+#pragma unroll
+            for (int i = 0; i < OT; ++i) o[i] *= f;
+            l *= f;
+            m = top;
+        }
+        half2_t p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float lift = m == -INFINITY ? 0.0f : m - P_LIFT;
+            const float x = __builtin_amdgcn_exp2f(s[2 * i] - lift), y = __builtin_amdgcn_exp2f(s[2 * i + 1] - lift);
+            l += x + y;
+            p[i] = half2_t{_Float16(x), _Float16(y)};
+        }
+        const uint4_t pw = {__builtin_bit_cast(uint32_t, p[0]), __builtin_bit_cast(uint32_t, p[1]), __builtin_bit_cast(uint32_t, p[2]),
+                            __builtin_bit_cast(uint32_t, p[3])};
+#pragma unroll
+        for (int x = 0; x < VH; ++x) {
+            // channels 64 x + 4 c16 + c of tokens t8 ..
+            const uint4 w = *reinterpret_cast<const uint4 *>(data + P::V + (((at >> 3) + g) * HD + 64 * x + 4 * c16) * 4);
+            uint2 bytes = *reinterpret_cast<const uint2 *>(data + P::VS + (2 * x + (c16 >> 3)) * FP4_PAGE + at + 8 * g);
+            // a token that no row sees may be any bits: no infinity times a weight of 0
+            if (t0 + FP4_STEP > steps.end || t0 < steps.begin) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int t = t8 + i;
+                    if (!(t < steps.end && (t >= steps.begin || t < a.sinks))) (i < 4 ? bytes.x : bytes.y) &= ~(255u << (8 * (i & 3)));
+                }
+            }
+            half2_t scale[4];
+            scale_pairs(bytes, scale);
+            const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) o[4 * x + c] = product16<false>(column_operand(words[c], scale), pw, o[4 * x + c]);
+        }
+    }
+
+    // The four waves' results: each scaled to their common maximum, then summed.  A lane's o[4x + c][i] is channel
+    // 64x + 16g + 4i + c.
+    l = column_sum(l);
+    if (g == 0) lds_m[wave][c16] = m, lds_l[wave][c16] = l;
+    __syncthreads();
+    const float top = fmaxf(fmaxf(lds_m[0][c16], lds_m[1][c16]), fmaxf(lds_m[2][c16], lds_m[3][c16]));
+    const float mine = weight_of(m, top);
+#pragma unroll
+    for (int x = 0; x < VH; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<float4 *>(&lds_o[wave][c16][64 * x + 16 * g + 4 * i]) =
+                make_float4(o[4 * x][i] * mine, o[4 * x + 1][i] * mine, o[4 * x + 2][i] * mine, o[4 * x + 3][i] * mine);
+    __syncthreads();
+    // sixteen threads to a column, four channels at a time
+    const int to = threadIdx.x >> 4, part = threadIdx.x & 15;
+    const int to_column = column0 + to;
+    const float to_m = fmaxf(fmaxf(lds_m[0][to], lds_m[1][to]), fmaxf(lds_m[2][to], lds_m[3][to]));
+    float to_l = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) to_l += lds_l[w][to] * weight_of(lds_m[w][to], to_m);
+    const int to_row = to_column / v.G;
+    const int64_t to_out = seq.first + to_row;
+    if (to_column >= columns || to_out < 0 || to_out >= v.n_rows) return;
+    const int64_t index = to_out * (int64_t(v.H) * v.G) + h * v.G + to_column % v.G;
+    float *rows = a.part ? a.part + (rest * a.splits + split) * FP4_COLUMNS * (HD + 4) + to * (HD + 4) : nullptr;
+    const float inverse = to_l > 0.0f || to_l != to_l ? 1.0f / to_l : 0.0f;
+#pragma unroll
+    for (int x = 0; x < VH; ++x) {
+        const int channel = 64 * x + 4 * part;
+        float r[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            r[i] = (lds_o[0][to][channel + i] + lds_o[1][to][channel + i]) + (lds_o[2][to][channel + i] + lds_o[3][to][channel + i]);
+        if (rows) {
+            *reinterpret_cast<float4 *>(rows + channel) = make_float4(r[0], r[1], r[2], r[3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] *= inverse;
+            store_out(a.out, a.out_type, index * HD + channel, r);
+        }
+    }
+    if (part == 0) {
+        if (rows) rows[HD] = to_m, rows[HD + 1] = to_l;
+        else if (a.lse) a.lse[index] = to_l > 0.0f || to_l != to_l ? (to_m - P_LIFT + __log2f(to_l)) * 0.6931471805599453f : -INFINITY;
+    }
+}
+
+// Joins the splits: a workgroup of HD threads to a column.
+template <int HD>
+__global__ __launch_bounds__(HD) void fp4_join_kernel(Fp4Attention a) {
+    const Fp4View &v = a.v;
+    const int c = int(blockIdx.x % FP4_COLUMNS);
+    const int64_t rest = blockIdx.x / FP4_COLUMNS;
+    const int h = int(rest % v.H), b = int(rest / v.H % v.batch.batch), block = int(rest / v.H / v.batch.batch);
+    const Fp4Sequence seq(v, b);
+    const int column = block * FP4_COLUMNS + c;
+    const int64_t out_row = seq.first + column / v.G;
+    if (column >= seq.n * v.G || out_row < 0 || out_row >= v.n_rows) return;
+    const float *rows = a.part + (rest * a.splits * FP4_COLUMNS + c) * (HD + 4);
+    const int64_t pitch = FP4_COLUMNS * (HD + 4);
+    float m = -INFINITY;
+    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, rows[s * pitch + HD]);
+    float l = 0.0f, o = 0.0f;
+    for (int s = 0; s < a.splits; ++s) {
+        const float f = weight_of(rows[s * pitch + HD], m);
+        l += f * rows[s * pitch + HD + 1];
+        o += f * rows[s * pitch + threadIdx.x];
+    }
+    const bool some = l > 0.0f || l != l;
+    const int64_t index = out_row * (int64_t(v.H) * v.G) + h * v.G + column % v.G;
+    const float r = some ? o / l : 0.0f;
+    const int64_t at = index * HD + threadIdx.x;
+    if (a.out_type == KV_TYPE_FP32) static_cast<float *>(a.out)[at] = r;
+    else if (a.out_type == KV_TYPE_BF16) static_cast<__bf16 *>(a.out)[at] = __bf16(r);
+    else static_cast<_Float16 *>(a.out)[at] = _Float16(r);
+    if (a.lse && threadIdx.x == 0) a.lse[index] = some ? (m - P_LIFT + __log2f(l)) * 0.6931471805599453f : -INFINITY;
+}
+
+int launch_fp4_attention(const kv_fp4_cache *c, const Fp4View &v, const void *q, int64_t q_stride, bool bf16, float sm_scale,
+                         int window, int sinks, void *out, int out_type, float *lse, hipStream_t s) {
+    const int64_t columns = int64_t(v.batch.max_new) * v.G;
+    if (columns > (int64_t(1) << 30)) return KV_ERR_UNSUPPORTED;
+    Fp4Attention a;
+    a.v = v;
+    a.q = static_cast<const uint16_t *>(q);
+    a.q_stride = q_stride;
+    a.scale = sm_scale * 1.4426950408889634f;
+    a.window = window, a.sinks = sinks;
+    a.out = out, a.out_type = out_type, a.lse = lse;
+    a.blocks = int((columns + FP4_COLUMNS - 1) / FP4_COLUMNS);
+    const int64_t streams = int64_t(a.blocks) * v.batch.batch * v.H;
+    // Steps that a block of columns can have.
+    int64_t most = int64_t(v.batch.table_pages) * (FP4_PAGE / FP4_STEP);
+    if (window) most = std::min(most, (int64_t(window) + FP4_COLUMNS + sinks) / FP4_STEP + 3);
+    int64_t splits = std::min<int64_t>({1024 / streams, (most + 7) / 8, FP4_SPLITS_MAX, FP4_PART_ROWS / FP4_COLUMNS / streams});
+    a.splits = int(std::max<int64_t>(splits, 1));
+    a.part = a.splits > 1 ? c->workspace : nullptr;
+    const int64_t groups = streams * a.splits;
+    if (groups > 0x7FFFFFFF || streams * FP4_COLUMNS > 0x7FFFFFFF) return KV_ERR_UNSUPPORTED;
+#define LAUNCH(HD, BF) hipLaunchKernelGGL((fp4_attention_kernel<HD, BF>), dim3(unsigned(groups)), dim3(256), 0, s, a)
+    if (c->cfg.head_dim == 128) {
+        if (bf16) LAUNCH(128, true); else LAUNCH(128, false);
+    } else {
+        if (bf16) LAUNCH(64, true); else LAUNCH(64, false);
+    }
+#undef LAUNCH
+    KV_HIP_CHECK(hipGetLastError());
+    if (a.splits > 1) {
+        const dim3 grid(unsigned(streams * FP4_COLUMNS));
+        if (c->cfg.head_dim == 128) hipLaunchKernelGGL(fp4_join_kernel<128>, grid, dim3(128), 0, s, a);
+        else hipLaunchKernelGGL(fp4_join_kernel<64>, grid, dim3(64), 0, s, a);
+        KV_HIP_CHECK(hipGetLastError());
+    }
+    return KV_OK;
+}
+
+}  // namespace packkv
