@@ -90,12 +90,20 @@ __device__ inline uint4_t column_operand(uint32_t w, const half2_t (&scale)[4]) 
 
 // Sum or maximum over the four lanes of a column (lane, lane ^ 16, lane ^ 32, lane ^ 48).
 __device__ inline float column_max(float x) {
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
+    uint32_t a = __float_as_uint(x), b = a;
+    swap_rows16(a, b);
+    x = fmaxf(__uint_as_float(a), __uint_as_float(b));
+    a = b = __float_as_uint(x);
+    swap_rows32(a, b);
+    return fmaxf(__uint_as_float(a), __uint_as_float(b));
 }
 __device__ inline float column_sum(float x) {
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
+    uint32_t a = __float_as_uint(x), b = a;
+    swap_rows16(a, b);
+    x = __uint_as_float(a) + __uint_as_float(b);
+    a = b = __float_as_uint(x);
+    swap_rows32(a, b);
+    return __uint_as_float(a) + __uint_as_float(b);
 }
 
 // exp2(a - b) where -inf - -inf means no weight.
@@ -138,12 +146,126 @@ struct Fp4Steps {
     __device__ inline int token(int step) const { return FP4_STEP * (step < sink_steps ? step : step - sink_steps + window_step); }
 };
 
-template <int HD, bool BF16>
-__global__ __launch_bounds__(256) void fp4_attention_kernel(Fp4Attention a) {
+// What a wave reads of a step: of K a lane's quarter of two tokens' rows, of V a word (or HD / 64 times four) of eight tokens.
+template <int HD>
+struct Fp4Stage {
     using P = Fp4Block<HD>;
-    constexpr int KW = HD / 32;          // words of K in a lane's quarter of a row; products of 32 channels
-    constexpr int VH = HD / 64;          // 16-byte pieces of V per lane
-    constexpr int OT = HD / 16;          // blocks of 16 channels
+    static constexpr int KW = HD / 32, VH = HD / 64;
+    uint32_t k[2][KW];
+    uint4 v[VH];
+    uint32_t ks[2];
+    uint2 vs[VH];
+    int t0, end;             // first token; tokens from `end` on are not there (0: the page is missing)
+
+    // block: the head's in the page; at: the step's first token in it
+    __device__ inline void load(const uint8_t *block, int at, int c16, int g) {
+        const uint8_t *kp = block + P::K + at * (HD / 2), *sp = block + P::KS + at * (HD / FP4_GROUP);
+        const int token = 8 * (c16 >> 2) + (c16 & 3);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            if constexpr (KW == 4) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(kp + (token + 4 * t) * (HD / 2) + g * (HD / 8));
+                k[t][0] = x.x, k[t][1] = x.y, k[t][2] = x.z, k[t][3] = x.w;
+            } else {
+                const uint2 x = *reinterpret_cast<const uint2 *>(kp + (token + 4 * t) * (HD / 2) + g * (HD / 8));
+                k[t][0] = x.x, k[t][1] = x.y;
+            }
+            ks[t] = sp[(token + 4 * t) * (HD / FP4_GROUP) + g * (HD / 4) / FP4_GROUP];
+        }
+        const uint8_t *vp = block + P::V + at * (HD / 2), *wp = block + P::VS + at;
+#pragma unroll
+        for (int x = 0; x < VH; ++x) {
+            // channels 64 x + 4 c16 .. of tokens at + 8g ..
+            v[x] = *reinterpret_cast<const uint4 *>(vp + (g * HD + 64 * x + 4 * c16) * 4);
+            vs[x] = *reinterpret_cast<const uint2 *>(wp + (2 * x + (c16 >> 3)) * FP4_PAGE + 8 * g);
+        }
+    }
+};
+
+// The columns of a wave's matrix products, its running softmax and its sums.
+template <int HD, bool BF16>
+struct Fp4Columns {
+    static constexpr int KW = HD / 32, VH = HD / 64, OT = HD / 16;
+    uint4_t q[KW];
+    float4_t o[OT];
+    float m, l;              // of the scores before they are scaled; of this lane's tokens
+    int hi, lo;              // last token that the column sees; first of its window
+    float scale;
+    int sinks, begin;
+
+    // edge (wave-uniform): there are tokens that not every column sees
+    __device__ inline void step(const Fp4Stage<HD> &in, int g, bool edge) {
+        float4_t s[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            s[t] = float4_t{0, 0, 0, 0};
+            const float ks = __uint_as_float(in.ks[t] << 23);
+#pragma unroll
+            for (int i = 0; i < KW; ++i) s[t] = product16<BF16>(row_operand<BF16>(in.k[t][i], ks), q[i], s[t]);
+        }
+        const int t8 = in.t0 + 8 * g;
+        if (edge) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int t = t8 + i;
+                if (!(t <= hi && t < in.end && (t >= lo || t < sinks))) s[i >> 2][i & 3] = -INFINITY;
+            }
+        }
+        float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+        top = column_max(top);
+        if (__any(top > m)) {
+            const float now = fmaxf(m, top);
+            const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - now) * scale);
+#pragma unroll
+            for (int i = 0; i < OT; ++i) o[i] *= f;
+            l *= f;
+            m = now;
+        }
+        const float lift = m == -INFINITY ? P_LIFT : P_LIFT - m * scale;
+        half2_t p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float x = __builtin_amdgcn_exp2f(fmaf(s[i >> 1][2 * (i & 1)], scale, lift));
+            const float y = __builtin_amdgcn_exp2f(fmaf(s[i >> 1][2 * (i & 1) + 1], scale, lift));
+            l += x + y;
+            p[i] = half2_t{_Float16(x), _Float16(y)};
+        }
+        const uint4_t pw = {__builtin_bit_cast(uint32_t, p[0]), __builtin_bit_cast(uint32_t, p[1]), __builtin_bit_cast(uint32_t, p[2]),
+                            __builtin_bit_cast(uint32_t, p[3])};
+#pragma unroll
+        for (int x = 0; x < VH; ++x) {
+            uint2 bytes = in.vs[x];
+            if (edge) {
+                // a token that no row sees may be any bits: no infinity times a weight of 0
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int t = t8 + i;
+                    if (!(t < in.end && (t >= begin || t < sinks))) (i < 4 ? bytes.x : bytes.y) &= ~(255u << (8 * (i & 3)));
+                }
+            }
+            half2_t vs[4];
+            scale_pairs(bytes, vs);
+            const uint32_t words[4] = {in.v[x].x, in.v[x].y, in.v[x].z, in.v[x].w};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) o[4 * x + c] = product16<false>(column_operand(words[c], vs), pw, o[4 * x + c]);
+        }
+    }
+};
+
+// The page numbers of the next 64 steps of a wave, one to a lane: none of its transfers waits for the table.
+struct Fp4Pages {
+    int page;                // (page numbers fit 31 bits) -1: missing
+    __device__ inline void load(const Fp4View &v, const Fp4Sequence &seq, const Fp4Steps &steps, int step, int end, int lane) {
+        const int mine = step + 4 * lane;
+        page = mine < end ? int(seq.page(v, steps.token(mine) / FP4_PAGE)) : -1;
+    }
+    __device__ inline int at(int i) const { return __builtin_amdgcn_readlane(page, i); }
+};
+
+template <int HD, bool BF16>
+__global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(Fp4Attention a) {
+    using P = Fp4Block<HD>;
+    constexpr int KW = HD / 32, VH = HD / 64, OT = HD / 16;
     __shared__ float lds_o[4][FP4_COLUMNS][HD + 4];
     __shared__ float lds_m[4][FP4_COLUMNS], lds_l[4][FP4_COLUMNS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c16 = lane & 15, g = lane >> 4;
@@ -157,97 +279,57 @@ __global__ __launch_bounds__(256) void fp4_attention_kernel(Fp4Attention a) {
     const Fp4Steps steps(seq, column0, FP4_COLUMNS, v.G, a.window, a.sinks);
     const int per_split = (steps.n + a.splits - 1) / a.splits;
     const int step_end = min((split + 1) * per_split, steps.n);
+    int step = __builtin_amdgcn_readfirstlane(split * per_split + wave);
 
     // this lane's column
     const int column = column0 + c16, row = column / v.G, head = h * v.G + column % v.G;
     const int64_t out_row = seq.first + row;
     const bool real = column < columns && out_row >= 0 && out_row < v.n_rows;
-    const int hi = max(seq.pos0 + row, -1), lo = a.window ? hi - a.window + 1 : 0;
-    uint4_t q[KW];
+    Fp4Columns<HD, BF16> col;
+    col.hi = max(seq.pos0 + row, -1), col.lo = a.window ? col.hi - a.window + 1 : 0;
+    col.sinks = a.sinks, col.begin = steps.begin;
+    // A negative scale is one of -q: the largest scaled score is then that of the largest score.  Scores are below 2^39, so
+    // below 1e-30 all that are seen weigh the same, as with 0 (which would make a NaN of a score that is not seen).
+    col.scale = fmaxf(fabsf(a.scale), 1e-30f);
+    const uint32_t sign = a.scale < 0.0f ? 0x80008000u : 0u;
 #pragma unroll
     for (int i = 0; i < KW; ++i) {
-        q[i] = uint4_t{0, 0, 0, 0};
-        if (real) q[i] = *reinterpret_cast<const uint4_t *>(a.q + out_row * a.q_stride + int64_t(head) * HD + g * (HD / 4) + 8 * i);
+        col.q[i] = uint4_t{0, 0, 0, 0};
+        if (real) col.q[i] = *reinterpret_cast<const uint4_t *>(a.q + out_row * a.q_stride + int64_t(head) * HD + g * (HD / 4) + 8 * i) ^ sign;
     }
+#pragma unroll
+    for (int i = 0; i < OT; ++i) col.o[i] = float4_t{0, 0, 0, 0};
+    col.m = -INFINITY, col.l = 0.0f;
+    // a step whose tokens every column of the block sees needs no masks
+    const int first_hi = max(seq.pos0 + steps.first_row, -1), last_lo = a.window ? max(seq.pos0 + steps.last_row - a.window + 1, 0) : 0;
 
-    float4_t o[OT];
-#pragma unroll
-    for (int i = 0; i < OT; ++i) o[i] = float4_t{0, 0, 0, 0};
-    float m = -INFINITY, l = 0.0f;
-
-    for (int step = split * per_split + wave; step < step_end; step += 4) {
-        const int t0 = steps.token(step);
-        const int64_t page = seq.page(v, t0 / FP4_PAGE);
-        if (page < 0) continue;
-        const uint8_t *data = v.pages + (page * v.H + h) * size_t(P::BYTES);
-        const int at = t0 % FP4_PAGE;
-        // scores of tokens t0 + 8g + 4t + i, i < 4, in s[t]
-        float s[8];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int token = at + 8 * (c16 >> 2) + 4 * t + (c16 & 3);
-            uint32_t w[KW];
-            const uint8_t *from = data + P::K + token * (HD / 2) + g * (HD / 8);
-            if constexpr (KW == 4) {
-                const uint4 x = *reinterpret_cast<const uint4 *>(from);
-                w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
-            } else {
-                const uint2 x = *reinterpret_cast<const uint2 *>(from);
-                w[0] = x.x, w[1] = x.y;
-            }
-            const float scale = __uint_as_float(uint32_t(data[P::KS + token * (HD / FP4_GROUP) + g * (HD / 4) / FP4_GROUP]) << 23);
-            float4_t acc = {0, 0, 0, 0};
-#pragma unroll
-            for (int i = 0; i < KW; ++i) acc = product16<BF16>(row_operand<BF16>(w[i], scale), q[i], acc);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[4 * t + i] = acc[i] * a.scale;
-        }
-        const int t8 = t0 + 8 * g;
-        float top = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int t = t8 + i;
-            if (!(t <= hi && t < steps.end && (t >= lo || t < a.sinks))) s[i] = -INFINITY;
-            top = fmaxf(top, s[i]);
-        }
-        top = column_max(top);
-        if (top > m) {
-            const float f = weight_of(m, top);
-#pragma unroll
-            for (int i = 0; i < OT; ++i) o[i] *= f;
-            l *= f;
-            m = top;
-        }
-        half2_t p[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float lift = m == -INFINITY ? 0.0f : m - P_LIFT;
-            const float x = __builtin_amdgcn_exp2f(s[2 * i] - lift), y = __builtin_amdgcn_exp2f(s[2 * i + 1] - lift);
-            l += x + y;
-            p[i] = half2_t{_Float16(x), _Float16(y)};
-        }
-        const uint4_t pw = {__builtin_bit_cast(uint32_t, p[0]), __builtin_bit_cast(uint32_t, p[1]), __builtin_bit_cast(uint32_t, p[2]),
-                            __builtin_bit_cast(uint32_t, p[3])};
-#pragma unroll
-        for (int x = 0; x < VH; ++x) {
-            // channels 64 x + 4 c16 + c of tokens t8 ..
-            const uint4 w = *reinterpret_cast<const uint4 *>(data + P::V + (((at >> 3) + g) * HD + 64 * x + 4 * c16) * 4);
-            uint2 bytes = *reinterpret_cast<const uint2 *>(data + P::VS + (2 * x + (c16 >> 3)) * FP4_PAGE + at + 8 * g);
-            // a token that no row sees may be any bits: no infinity times a weight of 0
-            if (t0 + FP4_STEP > steps.end || t0 < steps.begin) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int t = t8 + i;
-                    if (!(t < steps.end && (t >= steps.begin || t < a.sinks))) (i < 4 ? bytes.x : bytes.y) &= ~(255u << (8 * (i & 3)));
-                }
-            }
-            half2_t scale[4];
-            scale_pairs(bytes, scale);
-            const uint32_t words[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int c = 0; c < 4; ++c) o[4 * x + c] = product16<false>(column_operand(words[c], scale), pw, o[4 * x + c]);
+    Fp4Stage<HD> in[2];
+    Fp4Pages pages;
+    auto fetch = [&](Fp4Stage<HD> &to, int at_step) {
+        const int i = (at_step - step) >> 2;
+        const int page = pages.at(i);
+        to.t0 = steps.token(at_step);
+        to.end = page < 0 ? 0 : steps.end;
+        to.load(v.pages + (int64_t(max(page, 0)) * v.H + h) * size_t(P::BYTES), to.t0 % FP4_PAGE, c16, g);
+    };
+    auto compute = [&](const Fp4Stage<HD> &from) {
+        col.step(from, g, from.t0 + FP4_STEP > min(from.end, first_hi + 1) || from.t0 < last_lo);
+    };
+    for (; step < step_end; step += 4 * 64) {
+        pages.load(v, seq, steps, step, step_end, lane);
+        const int last = min(step_end, step + 4 * 64);
+        fetch(in[0], step);
+        for (int at = step; at < last; at += 8) {
+            if (at + 4 < last) fetch(in[1], at + 4);
+            compute(in[0]);
+            if (at + 4 >= last) break;
+            if (at + 8 < last) fetch(in[0], at + 8);
+            compute(in[1]);
         }
     }
+    float4_t(&o)[OT] = col.o;
+    float l = col.l;
+    const float m = col.m == -INFINITY ? col.m : col.m * col.scale;
 
     // The four waves' results: each scaled to their common maximum, then summed.  A lane's o[4x + c][i] is channel
     // 64x + 16g + 4i + c.
@@ -297,11 +379,14 @@ __global__ __launch_bounds__(256) void fp4_attention_kernel(Fp4Attention a) {
     }
 }
 
-// Joins the splits: a workgroup of HD threads to a column.
+// Joins the splits: a workgroup to a column.  Threads first read a split's maximum each, then sum rows: HD / 4 threads to a
+// row, four channels each, eight (sixteen) rows at a time.
 template <int HD>
-__global__ __launch_bounds__(HD) void fp4_join_kernel(Fp4Attention a) {
+__global__ __launch_bounds__(256) void fp4_join_kernel(Fp4Attention a) {
+    constexpr int PARTS = 256 / (HD / 4);
+    __shared__ float weight[FP4_SPLITS_MAX], sums[PARTS][HD + 4], shared[4];
     const Fp4View &v = a.v;
-    const int c = int(blockIdx.x % FP4_COLUMNS);
+    const int c = int(blockIdx.x % FP4_COLUMNS), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t rest = blockIdx.x / FP4_COLUMNS;
     const int h = int(rest % v.H), b = int(rest / v.H % v.batch.batch), block = int(rest / v.H / v.batch.batch);
     const Fp4Sequence seq(v, b);
@@ -310,14 +395,37 @@ __global__ __launch_bounds__(HD) void fp4_join_kernel(Fp4Attention a) {
     if (column >= seq.n * v.G || out_row < 0 || out_row >= v.n_rows) return;
     const float *rows = a.part + (rest * a.splits * FP4_COLUMNS + c) * (HD + 4);
     const int64_t pitch = FP4_COLUMNS * (HD + 4);
-    float m = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, rows[s * pitch + HD]);
-    float l = 0.0f, o = 0.0f;
-    for (int s = 0; s < a.splits; ++s) {
-        const float f = weight_of(rows[s * pitch + HD], m);
-        l += f * rows[s * pitch + HD + 1];
-        o += f * rows[s * pitch + threadIdx.x];
+    const int s = threadIdx.x;
+    static_assert(FP4_SPLITS_MAX <= 256, "a thread to a split");
+    const float my_m = s < a.splits ? rows[s * pitch + HD] : -INFINITY, my_l = s < a.splits ? rows[s * pitch + HD + 1] : 0.0f;
+    const int part = threadIdx.x / (HD / 4), four = threadIdx.x % (HD / 4);
+    float m = my_m;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    if (lane == 0) shared[wave] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(shared[0], shared[1]), fmaxf(shared[2], shared[3]));
+    const float f = weight_of(my_m, m);
+    weight[s] = f;
+    float l = my_l * f;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) l += __shfl_xor(l, d);
+    __syncthreads();
+    if (lane == 0) shared[wave] = l;
+    float4 acc = make_float4(0, 0, 0, 0);
+#pragma unroll 4
+    for (int i = part; i < a.splits; i += PARTS) {
+        const float4 x = *reinterpret_cast<const float4 *>(rows + i * pitch + 4 * four);
+        const float w = weight[i];
+        acc.x = fmaf(w, x.x, acc.x), acc.y = fmaf(w, x.y, acc.y), acc.z = fmaf(w, x.z, acc.z), acc.w = fmaf(w, x.w, acc.w);
     }
+    *reinterpret_cast<float4 *>(&sums[part][4 * four]) = acc;
+    __syncthreads();
+    if (threadIdx.x >= HD) return;
+    l = (shared[0] + shared[1]) + (shared[2] + shared[3]);
+    float o = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) o += sums[i][threadIdx.x];
     const bool some = l > 0.0f || l != l;
     const int64_t index = out_row * (int64_t(v.H) * v.G) + h * v.G + column % v.G;
     const float r = some ? o / l : 0.0f;
@@ -359,8 +467,8 @@ int launch_fp4_attention(const kv_fp4_cache *c, const Fp4View &v, const void *q,
     KV_HIP_CHECK(hipGetLastError());
     if (a.splits > 1) {
         const dim3 grid(unsigned(streams * FP4_COLUMNS));
-        if (c->cfg.head_dim == 128) hipLaunchKernelGGL(fp4_join_kernel<128>, grid, dim3(128), 0, s, a);
-        else hipLaunchKernelGGL(fp4_join_kernel<64>, grid, dim3(64), 0, s, a);
+        if (c->cfg.head_dim == 128) hipLaunchKernelGGL(fp4_join_kernel<128>, grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL(fp4_join_kernel<64>, grid, dim3(256), 0, s, a);
         KV_HIP_CHECK(hipGetLastError());
     }
     return KV_OK;
