@@ -470,7 +470,7 @@ int kv_fp4_read(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, void *k, voi
  * left as they were.
  * q.Khat: exact products on the matrix cores, fp32 sums; softmax in fp32; its weights
  * enter the product with Vhat as fp16 (scaled by a power of two: a relative error of
- * at most 2^-11 down to 2^-29 of the row's largest weight), sums in fp32.  A NaN or
+ * at most 2^-11 down to 2^-26 of the row's largest weight), sums in fp32.  A NaN or
  * infinity in q stays with its row and head.  Sums have a fixed order: the result
  * is bitwise reproducible.  Uses the workspace: attention calls on one cache must not overlap.
  */

@@ -24,8 +24,10 @@ typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
 
 constexpr int FP4_STEP = 32;             // tokens of a step: half a page
 constexpr int FP4_COLUMNS = 16;
-// Weights are held as 2^P_LIFT times their size: the largest is then 2^15, and fp16 keeps its eleven bits down to 2^-29.
-constexpr float P_LIFT = 15.0f;
+// Weights are relative to a maximum that follows the scores only when one is P_SLACK (in powers of two) above it: most steps
+// scale no sums then.  They are held as 2^P_LIFT times their size, so that the largest is between 2^12 and 2^15, and fp16
+// keeps its eleven bits down to 2^-26 of it.
+constexpr float P_LIFT = 12.0f, P_SLACK = 3.0f;
 // Partial results: at most so many rows (of a column in a split) of HD + 4 floats.
 constexpr int64_t FP4_PART_ROWS = 32768;
 constexpr int FP4_SPLITS_MAX = 256;
@@ -88,7 +90,7 @@ __device__ inline uint4_t column_operand(uint32_t w, const half2_t (&scale)[4]) 
     return r;
 }
 
-// Sum or maximum over the four lanes of a column (lane, lane ^ 16, lane ^ 32, lane ^ 48).
+// Maximum and sum over the four lanes of a column (lane, lane ^ 16, lane ^ 32, lane ^ 48).
 __device__ inline float column_max(float x) {
     uint32_t a = __float_as_uint(x), b = a;
     swap_rows16(a, b);
@@ -97,6 +99,7 @@ __device__ inline float column_max(float x) {
     swap_rows32(a, b);
     return fmaxf(__uint_as_float(a), __uint_as_float(b));
 }
+
 __device__ inline float column_sum(float x) {
     uint32_t a = __float_as_uint(x), b = a;
     swap_rows16(a, b);
@@ -104,6 +107,12 @@ __device__ inline float column_sum(float x) {
     a = b = __float_as_uint(x);
     swap_rows32(a, b);
     return __uint_as_float(a) + __uint_as_float(b);
+}
+
+__device__ inline float max3(float a, float b, float c) {   // (without the instructions that quiet a signalling NaN first)
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
 }
 
 // exp2(a - b) where -inf - -inf means no weight.
@@ -188,10 +197,18 @@ struct Fp4Columns {
     static constexpr int KW = HD / 32, VH = HD / 64, OT = HD / 16;
     uint4_t q[KW];
     float4_t o[OT];
-    float m, l;              // of the scores before they are scaled; of this lane's tokens
+    float l, m, bar, lift;   // sum of this lane's weights; what the weights are relative to; score that moves it; P_LIFT - m * scale
     int hi, lo;              // last token that the column sees; first of its window
-    float scale;
+    float scale, slack;      // slack: P_SLACK / scale
     int sinks, begin;
+
+    __device__ inline void clear() {
+#pragma unroll
+        for (int i = 0; i < OT; ++i) o[i] = float4_t{0, 0, 0, 0};
+        l = 0.0f;
+        m = bar = -INFINITY;
+        lift = P_LIFT;
+    }
 
     // edge (wave-uniform): there are tokens that not every column sees
     __device__ inline void step(const Fp4Stage<HD> &in, int g, bool edge) {
@@ -203,25 +220,36 @@ struct Fp4Columns {
 #pragma unroll
             for (int i = 0; i < KW; ++i) s[t] = product16<BF16>(row_operand<BF16>(in.k[t][i], ks), q[i], s[t]);
         }
-        const int t8 = in.t0 + 8 * g;
+        uint2 vs[VH];
+#pragma unroll
+        for (int x = 0; x < VH; ++x) vs[x] = in.vs[x];
         if (edge) {
+            uint32_t keep[2] = {0, 0};
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int t = t8 + i;
-                if (!(t <= hi && t < in.end && (t >= lo || t < sinks))) s[i >> 2][i & 3] = -INFINITY;
+                const int t = in.t0 + 8 * g + i;
+                const bool ok = (t <= hi) & (t < in.end) & ((t >= lo) | (t < sinks));
+                s[i >> 2][i & 3] = ok ? s[i >> 2][i & 3] : -INFINITY;
+                // a token that no row sees may be any bits: no infinity times a weight of 0
+                const bool seen = (t < in.end) & ((t >= begin) | (t < sinks));
+                keep[i >> 2] |= seen ? 255u << (8 * (i & 3)) : 0u;
+            }
+#pragma unroll
+            for (int x = 0; x < VH; ++x) vs[x].x &= keep[0], vs[x].y &= keep[1];
+        }
+        float top = max3(max3(s[0][0], s[0][1], s[0][2]), max3(s[0][3], s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]));
+        if (__any(top > bar)) {
+            top = column_max(top);
+            if (top > bar) {
+                const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - top) * scale);
+#pragma unroll
+                for (int i = 0; i < OT; ++i) o[i] *= f;
+                l *= f;
+                m = top;
+                bar = top + slack;
+                lift = P_LIFT - top * scale;
             }
         }
-        float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-        top = column_max(top);
-        if (__any(top > m)) {
-            const float now = fmaxf(m, top);
-            const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - now) * scale);
-#pragma unroll
-            for (int i = 0; i < OT; ++i) o[i] *= f;
-            l *= f;
-            m = now;
-        }
-        const float lift = m == -INFINITY ? P_LIFT : P_LIFT - m * scale;
         half2_t p[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -234,20 +262,11 @@ struct Fp4Columns {
                             __builtin_bit_cast(uint32_t, p[3])};
 #pragma unroll
         for (int x = 0; x < VH; ++x) {
-            uint2 bytes = in.vs[x];
-            if (edge) {
-                // a token that no row sees may be any bits: no infinity times a weight of 0
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int t = t8 + i;
-                    if (!(t < in.end && (t >= begin || t < sinks))) (i < 4 ? bytes.x : bytes.y) &= ~(255u << (8 * (i & 3)));
-                }
-            }
-            half2_t vs[4];
-            scale_pairs(bytes, vs);
+            half2_t scales[4];
+            scale_pairs(vs[x], scales);
             const uint32_t words[4] = {in.v[x].x, in.v[x].y, in.v[x].z, in.v[x].w};
 #pragma unroll
-            for (int c = 0; c < 4; ++c) o[4 * x + c] = product16<false>(column_operand(words[c], vs), pw, o[4 * x + c]);
+            for (int c = 0; c < 4; ++c) o[4 * x + c] = product16<false>(column_operand(words[c], scales), pw, o[4 * x + c]);
         }
     }
 };
@@ -297,9 +316,8 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(F
         col.q[i] = uint4_t{0, 0, 0, 0};
         if (real) col.q[i] = *reinterpret_cast<const uint4_t *>(a.q + out_row * a.q_stride + int64_t(head) * HD + g * (HD / 4) + 8 * i) ^ sign;
     }
-#pragma unroll
-    for (int i = 0; i < OT; ++i) col.o[i] = float4_t{0, 0, 0, 0};
-    col.m = -INFINITY, col.l = 0.0f;
+    col.slack = P_SLACK / col.scale;
+    col.clear();
     // a step whose tokens every column of the block sees needs no masks
     const int first_hi = max(seq.pos0 + steps.first_row, -1), last_lo = a.window ? max(seq.pos0 + steps.last_row - a.window + 1, 0) : 0;
 
@@ -318,22 +336,23 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(F
     for (; step < step_end; step += 4 * 64) {
         pages.load(v, seq, steps, step, step_end, lane);
         const int last = min(step_end, step + 4 * 64);
+        const int most = last - 1 - (last - 1 - step) % 4;      // the wave's last step of these
+        // Every fetch is made, behind the last one of that step again: a transfer that is made on some paths only would have
+        // the next use of any wait for all of them.
         fetch(in[0], step);
         for (int at = step; at < last; at += 8) {
-            if (at + 4 < last) fetch(in[1], at + 4);
+            fetch(in[1], min(at + 4, most));
             compute(in[0]);
             if (at + 4 >= last) break;
-            if (at + 8 < last) fetch(in[0], at + 8);
+            fetch(in[0], min(at + 8, most));
             compute(in[1]);
         }
     }
     float4_t(&o)[OT] = col.o;
-    float l = col.l;
-    const float m = col.m == -INFINITY ? col.m : col.m * col.scale;
+    const float l = column_sum(col.l), m = col.m == -INFINITY ? col.m : col.m * col.scale;
 
     // The four waves' results: each scaled to their common maximum, then summed.  A lane's o[4x + c][i] is channel
     // 64x + 16g + 4i + c.
-    l = column_sum(l);
     if (g == 0) lds_m[wave][c16] = m, lds_l[wave][c16] = l;
     __syncthreads();
     const float top = fmaxf(fmaxf(lds_m[0][c16], lds_m[1][c16]), fmaxf(lds_m[2][c16], lds_m[3][c16]));

@@ -62,7 +62,8 @@ def attention(q, k, v, n, sm_scale, window=0, sinks=0, present=None):
 
     It is allowed: products of q and k exact, D of them summed in fp32 in any order (each addition off by 2^-24 of the sum of
     magnitudes), the score scaled and its exponential taken with a few roundings more; weights rounded to fp16, half a step
-    2^-11 of their size (below 2^-29 of the row's largest: 2^-40 of that); sums over the tokens in fp32, in blocks."""
+    2^-11 of their size (below 2^-26 of the row's largest: 2^-37 of that, half of fp16's least step 2^-24 where the largest is held as
+    2^12 or more); sums over the tokens in fp32, in blocks."""
     length, H, D = k.shape
     G = q.shape[1] // H
     ok = seen(length, n, window, sinks)
@@ -86,6 +87,6 @@ def attention(q, k, v, n, sm_scale, window=0, sinks=0, present=None):
     sums = (length / 8 + 64) * 2.0 ** -24
     around = torch.einsum("nht,thd->nhd", p, vv.abs())
     bound = around * (2.0 ** -11 + 2 * score + 2 * sums)[..., None]
-    bound += 2.0 ** -40 * torch.einsum("nht,thd->nhd", ok[:, None, :].double().expand_as(p), vv.abs())
+    bound += 2.0 ** -37 * torch.einsum("nht,thd->nhd", ok[:, None, :].double().expand_as(p), vv.abs())
     lse_bound = score + sums + 2.0 ** -21 * (1 + lse.abs())
     return out, lse, bound, lse_bound
