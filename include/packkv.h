@@ -415,7 +415,7 @@ typedef struct {
  * and at position lens[b] - new_rows[b] + i of the sequence.  All arrays are device
  * memory.  Rows outside the tensors are left out. */
 typedef struct {
-    int32_t batch;             /* sequences >= 1                                  */
+    int32_t batch;             /* sequences, 1 .. 65535                           */
     int32_t max_new;           /* most new rows of a sequence; new_rows above it count as it */
     int32_t table_pages;       /* pages of a sequence at most: 1 .. 2^24          */
     const int32_t *lens;       /* [batch], negative: 0                            */

@@ -82,7 +82,8 @@ EXPORTS = ("kv_query_sizes", "kv_cache_create", "kv_cache_destroy", "kv_compress
            "kv_fp4_attention")
 # entry points the native module calls, in its order
 _NATIVE_CALLS = ("kv_compress_append", "kv_compress_append_bf16", "kv_k_matvec", "kv_softmax", "kv_v_matvec",
-                 "kv_decode_attention", "kv_cache_restore", "kv_cache_release", "kv_cache_tokens")
+                 "kv_decode_attention", "kv_cache_restore", "kv_cache_release", "kv_cache_tokens", "kv_fp4_append", "kv_fp4_read",
+                 "kv_fp4_attention")
 
 _lib = None
 _native = None
@@ -118,7 +119,7 @@ class _PythonCalls:
     def append(self, *args):
         return NotImplemented
 
-    k_matvec = softmax = v_matvec = attention = restore = release = append
+    k_matvec = softmax = v_matvec = attention = restore = release = read = append
 
 
 def lib():
@@ -470,7 +471,7 @@ class FP4Batch:
         self.lens, self.new_rows, self.first_row, self.page_table = lens, new_rows, first_row, page_table
         self._c = kv_fp4_batch_t(self.batch, self.max_new, self.table_pages,
                                  *(None if t is None else t.data_ptr() for t in (lens, new_rows, first_row, page_table)))
-        self._ref = C.byref(self._c)
+        self._ref, self._address, self._on = C.byref(self._c), C.addressof(self._c), self.device.index
 
 
 class FP4KVCache:
@@ -488,11 +489,14 @@ class FP4KVCache:
         handle = C.c_void_p()
         _check(lib().kv_fp4_cache_create(C.byref(self.cfg), self.pages.data_ptr(), self.workspace.data_ptr(),
                                          C.byref(sizes), C.byref(handle)), "kv_fp4_cache_create")
+        self._calls = _native.FP4Calls(n_kv_heads, n_q_heads, head_dim, str(self.device)) if _native else _PythonCalls()
         self.handle = handle
+        self._calls.set_handle(handle.value)
         self.n_pages, self.n_kv_heads, self.n_q_heads, self.head_dim = n_pages, n_kv_heads, n_q_heads, head_dim
 
     def close(self):
         if getattr(self, "handle", None) and _lib is not None:
+            self._calls.set_handle(0)
             _lib.kv_fp4_cache_destroy(self.handle)
         self.handle = None
 
@@ -540,6 +544,8 @@ class FP4KVCache:
 
     def kv_fp4_append(self, k, v, batch, stream=None):
         """k, v: fp16 or bf16 [rows, H_kv, D] (or [batch, n, H_kv, D]); may be parts of wider rows."""
+        if self._calls.append(k, v, batch._address, batch._on, stream) is not NotImplemented:
+            return
         half = (torch.float16, torch.bfloat16)
         rows, k_stride = self._rows("kv_fp4_append", k, self.n_kv_heads, half)
         v_rows, v_stride = self._rows("kv_fp4_append", v, self.n_kv_heads, half)
@@ -550,6 +556,10 @@ class FP4KVCache:
 
     def kv_fp4_read(self, batch, n_rows, dtype=torch.float16, k=None, v=None, stream=None):
         """The batch's new rows as the cache holds them: (k, v), [n_rows, H_kv, D] of dtype; rows of no sequence are not written."""
+        if k is None and v is None:
+            done = self._calls.read(batch._address, batch._on, n_rows, dtype, stream)
+            if done is not NotImplemented:
+                return done
         what, shape = "kv_fp4_read", (n_rows, self.n_kv_heads, self.head_dim)
         if dtype not in _TYPES:
             _refuse(what, "dtype is float16, bfloat16 or float32")
@@ -564,6 +574,10 @@ class FP4KVCache:
     def kv_fp4_attention(self, q, batch, sm_scale, window=0, sinks=0, out=None, lse=None, stream=None):
         """q: fp16 or bf16 [rows, H_q, D] (or [batch, n, H_q, D]) -> out [rows, H_q, D] of q's type (or of out's: fp16, bf16,
         fp32); lse: fp32 [rows, H_q] that gets the logarithms of the softmax sums.  Rows of no sequence are not written."""
+        if out is None and lse is None:
+            done = self._calls.attention(q, batch._address, batch._on, sm_scale, window, sinks, stream)
+            if done is not NotImplemented:
+                return done
         what = "kv_fp4_attention"
         rows, q_stride = self._rows(what, q, self.n_q_heads, (torch.float16, torch.bfloat16))
         if out is None:

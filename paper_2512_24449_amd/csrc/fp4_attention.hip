@@ -43,8 +43,12 @@ struct Fp4Attention {
     void *out;
     int out_type;
     float *lse;
-    float *part;             // [(column block, kv-head, sequence)][split][column]: HD sums, maximum, sum; null: one split
+    float *part;             // partial results, HD sums, maximum and sum of weights each; null: one split
     int splits, blocks;      // splits of the context, column blocks
+
+    __device__ inline int64_t part_row(int b, uint32_t stream, int split, int column) const {
+        return ((int64_t(b) * blocks * v.H + stream) * splits + split) * FP4_COLUMNS + column;
+    }
 };
 
 // Four words of a row (32 values' codes, HD / 4 of a lane) as operands: value pairs in the order of the channels.
@@ -289,9 +293,9 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(F
     __shared__ float lds_m[4][FP4_COLUMNS], lds_l[4][FP4_COLUMNS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c16 = lane & 15, g = lane >> 4;
     const Fp4View &v = a.v;
-    const int split = int(blockIdx.x % a.splits);
-    const int64_t rest = blockIdx.x / a.splits;
-    const int h = int(rest % v.H), b = int(rest / v.H % v.batch.batch), block = int(rest / v.H / v.batch.batch);
+    const uint32_t stream = blockIdx.x / uint32_t(a.splits);   // (block of columns, kv-head)
+    const int split = int(blockIdx.x - stream * a.splits), b = blockIdx.y;
+    const int block = int(stream / uint32_t(v.H)), h = int(stream - block * v.H);
     const Fp4Sequence seq(v, b);
     const int column0 = block * FP4_COLUMNS, columns = seq.n * v.G;
     if (column0 >= columns) return;
@@ -375,7 +379,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(F
     const int64_t to_out = seq.first + to_row;
     if (to_column >= columns || to_out < 0 || to_out >= v.n_rows) return;
     const int64_t index = to_out * (int64_t(v.H) * v.G) + h * v.G + to_column % v.G;
-    float *rows = a.part ? a.part + (rest * a.splits + split) * FP4_COLUMNS * (HD + 4) + to * (HD + 4) : nullptr;
+    float *rows = a.part ? a.part + a.part_row(b, stream, split, to) * (HD + 4) : nullptr;
     const float inverse = to_l > 0.0f || to_l != to_l ? 1.0f / to_l : 0.0f;
 #pragma unroll
     for (int x = 0; x < VH; ++x) {
@@ -405,14 +409,12 @@ __global__ __launch_bounds__(256) void fp4_join_kernel(Fp4Attention a) {
     constexpr int PARTS = 256 / (HD / 4);
     __shared__ float weight[FP4_SPLITS_MAX], sums[PARTS][HD + 4], shared[4];
     const Fp4View &v = a.v;
-    const int c = int(blockIdx.x % FP4_COLUMNS), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t rest = blockIdx.x / FP4_COLUMNS;
-    const int h = int(rest % v.H), b = int(rest / v.H % v.batch.batch), block = int(rest / v.H / v.batch.batch);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int column = int(blockIdx.x / uint32_t(v.H)), h = int(blockIdx.x - column * v.H), b = blockIdx.y;
     const Fp4Sequence seq(v, b);
-    const int column = block * FP4_COLUMNS + c;
     const int64_t out_row = seq.first + column / v.G;
     if (column >= seq.n * v.G || out_row < 0 || out_row >= v.n_rows) return;
-    const float *rows = a.part + (rest * a.splits * FP4_COLUMNS + c) * (HD + 4);
+    const float *rows = a.part + a.part_row(b, column / FP4_COLUMNS * v.H + h, 0, column % FP4_COLUMNS) * (HD + 4);
     const int64_t pitch = FP4_COLUMNS * (HD + 4);
     const int s = threadIdx.x;
     static_assert(FP4_SPLITS_MAX <= 256, "a thread to a split");
@@ -474,9 +476,10 @@ int launch_fp4_attention(const kv_fp4_cache *c, const Fp4View &v, const void *q,
     int64_t splits = std::min<int64_t>({1024 / streams, (most + 7) / 8, FP4_SPLITS_MAX, FP4_PART_ROWS / FP4_COLUMNS / streams});
     a.splits = int(std::max<int64_t>(splits, 1));
     a.part = a.splits > 1 ? c->workspace : nullptr;
-    const int64_t groups = streams * a.splits;
-    if (groups > 0x7FFFFFFF || streams * FP4_COLUMNS > 0x7FFFFFFF) return KV_ERR_UNSUPPORTED;
-#define LAUNCH(HD, BF) hipLaunchKernelGGL((fp4_attention_kernel<HD, BF>), dim3(unsigned(groups)), dim3(256), 0, s, a)
+    const int64_t groups = int64_t(a.blocks) * v.H * a.splits;
+    if (groups > 0x7FFFFFFF || columns * v.H > 0x7FFFFFFF) return KV_ERR_UNSUPPORTED;
+    const dim3 grid(unsigned(groups), unsigned(v.batch.batch));
+#define LAUNCH(HD, BF) hipLaunchKernelGGL((fp4_attention_kernel<HD, BF>), grid, dim3(256), 0, s, a)
     if (c->cfg.head_dim == 128) {
         if (bf16) LAUNCH(128, true); else LAUNCH(128, false);
     } else {
@@ -485,7 +488,7 @@ int launch_fp4_attention(const kv_fp4_cache *c, const Fp4View &v, const void *q,
 #undef LAUNCH
     KV_HIP_CHECK(hipGetLastError());
     if (a.splits > 1) {
-        const dim3 grid(unsigned(streams * FP4_COLUMNS));
+        const dim3 grid(unsigned(columns * v.H), unsigned(v.batch.batch));
         if (c->cfg.head_dim == 128) hipLaunchKernelGGL(fp4_join_kernel<128>, grid, dim3(256), 0, s, a);
         else hipLaunchKernelGGL(fp4_join_kernel<64>, grid, dim3(256), 0, s, a);
         KV_HIP_CHECK(hipGetLastError());

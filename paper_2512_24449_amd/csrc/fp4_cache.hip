@@ -96,10 +96,9 @@ __global__ __launch_bounds__(256) void fp4_append_kernel(Fp4View v, const uint16
     using T = Fp4Tile<HD>;
     using P = Fp4Block<HD>;
     const int lane = threadIdx.x & 63;
-    const int64_t unit = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (unit >= int64_t(tiles) * v.batch.batch * v.H) return;
-    const int h = int(unit % v.H);
-    const int tile = int(unit / v.H % tiles), b = int(unit / v.H / tiles);
+    const uint32_t unit = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int tile = int(unit / uint32_t(v.H)), h = int(unit - tile * v.H), b = blockIdx.y;
+    if (tile >= tiles) return;
     const Fp4Sequence seq(v, b);
     const int begin = max(seq.pos0, 0);                        // first position of the sequence that is written
     const int64_t start = (int64_t(begin / T::TOKENS) + tile) * T::TOKENS;
@@ -196,10 +195,9 @@ __global__ __launch_bounds__(256) void fp4_read_kernel(Fp4View v, uint8_t *__res
     using P = Fp4Block<HD>;
     constexpr int SIZE = TYPE == KV_TYPE_FP32 ? 4 : 2;
     const int lane = threadIdx.x & 63;
-    const int64_t unit = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (unit >= int64_t(tiles) * v.batch.batch * v.H) return;
-    const int h = int(unit % v.H);
-    const int tile = int(unit / v.H % tiles), b = int(unit / v.H / tiles);
+    const uint32_t unit = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int tile = int(unit / uint32_t(v.H)), h = int(unit - tile * v.H), b = blockIdx.y;
+    if (tile >= tiles) return;
     const Fp4Sequence seq(v, b);
     // positions may be negative here: tiles are aligned to multiples of TOKENS below them too
     const int64_t t0 = (seq.pos0 & ~(T::TOKENS - 1)) + int64_t(tile) * T::TOKENS;
@@ -248,10 +246,11 @@ inline int tiles_touched(int max_new, int tokens) { return int((int64_t(max_new)
 int launch_fp4_append(const kv_fp4_cache *c, const Fp4View &v, const void *k, int64_t k_stride, const void *vv, int64_t v_stride,
                       bool bf16, hipStream_t s) {
     const int tiles = tiles_touched(v.batch.max_new, c->cfg.head_dim == 128 ? Fp4Tile<128>::TOKENS : Fp4Tile<64>::TOKENS);
-    const int64_t groups = (int64_t(tiles) * v.batch.batch * v.H + 3) / 4;
-    if (groups > 0x7FFFFFFF) return KV_ERR_UNSUPPORTED;
+    const int64_t groups = (int64_t(tiles) * v.H + 3) / 4;
+    if (groups > 0x1FFFFFFF) return KV_ERR_UNSUPPORTED;
+    const dim3 grid(unsigned(groups), unsigned(v.batch.batch));
 #define LAUNCH(HD, BF)                                                                                                    \
-    hipLaunchKernelGGL((fp4_append_kernel<HD, BF>), dim3(unsigned(groups)), dim3(256), 0, s, v, static_cast<const uint16_t *>(k), \
+    hipLaunchKernelGGL((fp4_append_kernel<HD, BF>), grid, dim3(256), 0, s, v, static_cast<const uint16_t *>(k), \
                        k_stride, static_cast<const uint16_t *>(vv), v_stride, tiles)
     if (c->cfg.head_dim == 128) {
         if (bf16) LAUNCH(128, true); else LAUNCH(128, false);
@@ -265,10 +264,11 @@ int launch_fp4_append(const kv_fp4_cache *c, const Fp4View &v, const void *k, in
 
 int launch_fp4_read(const kv_fp4_cache *c, const Fp4View &v, void *k, void *vv, int type, hipStream_t s) {
     const int tiles = tiles_touched(v.batch.max_new, c->cfg.head_dim == 128 ? Fp4Tile<128>::TOKENS : Fp4Tile<64>::TOKENS);
-    const int64_t groups = (int64_t(tiles) * v.batch.batch * v.H + 3) / 4;
-    if (groups > 0x7FFFFFFF) return KV_ERR_UNSUPPORTED;
+    const int64_t groups = (int64_t(tiles) * v.H + 3) / 4;
+    if (groups > 0x1FFFFFFF) return KV_ERR_UNSUPPORTED;
+    const dim3 grid(unsigned(groups), unsigned(v.batch.batch));
 #define LAUNCH(HD, TYPE)                                                                                                  \
-    hipLaunchKernelGGL((fp4_read_kernel<HD, TYPE>), dim3(unsigned(groups)), dim3(256), 0, s, v, static_cast<uint8_t *>(k), \
+    hipLaunchKernelGGL((fp4_read_kernel<HD, TYPE>), grid, dim3(256), 0, s, v, static_cast<uint8_t *>(k), \
                        static_cast<uint8_t *>(vv), tiles)
 #define LAUNCH_TYPE(HD)                                                     \
     switch (type) {                                                         \
@@ -308,7 +308,7 @@ int check_batch(const kv_fp4_batch_t *b) {
     for (const void *p : {static_cast<const void *>(b->lens), static_cast<const void *>(b->new_rows),
                           static_cast<const void *>(b->first_row), static_cast<const void *>(b->page_table)})
         if (p && !aligned(p, 4)) return KV_ERR_ARG;
-    if (b->table_pages > (1 << 24)) return KV_ERR_UNSUPPORTED;
+    if (b->table_pages > (1 << 24) || b->batch > 65535) return KV_ERR_UNSUPPORTED;
     return KV_OK;
 }
 

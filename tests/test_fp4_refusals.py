@@ -66,7 +66,7 @@ def batch(**change):
 
 BAD_BATCHES = [(dict(batch=0), ARG), (dict(max_new=-1), ARG), (dict(table_pages=0), ARG), (dict(lens=None), ARG),
                (dict(lens=SOME + 2), ARG), (dict(new_rows=SOME + 1), ARG), (dict(first_row=SOME + 2), ARG),
-               (dict(page_table=SOME + 3), ARG), (dict(table_pages=2 ** 24 + 1), UNSUPPORTED)]
+               (dict(page_table=SOME + 3), ARG), (dict(table_pages=2 ** 24 + 1), UNSUPPORTED), (dict(batch=65536), UNSUPPORTED)]
 
 
 @pytest.mark.parametrize("change, want", BAD_BATCHES)
@@ -146,6 +146,7 @@ def test_binding_batches():
 def python_cache(cache):
     """The binding's object around the handle, its tensors on the CPU: what it refuses never reaches the library."""
     c = binding.FP4KVCache.__new__(binding.FP4KVCache)
+    c._calls = binding._PythonCalls()
     c.handle, c.device, c.n_pages, c.n_kv_heads, c.n_q_heads, c.head_dim = cache, torch.device("cpu"), 5, 2, 4, 128
     yield c
     c.handle = None

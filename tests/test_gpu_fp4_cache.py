@@ -232,3 +232,33 @@ def test_far_pages():
     cache.kv_fp4_append(x.to(DEV), x.to(DEV), batch)
     got = cache.kv_fp4_read(batch, 3)
     assert equal(got[0], ref.quantise(x)[0]) and equal(got[1], ref.quantise(x)[0])
+
+
+def test_native_calls_and_python_calls_agree():
+    """The binding's two ways of making a call give the same, for the layouts that one of them leaves to the other too."""
+    H, D, B, n = 2, 128, 2, 9
+    qkv = rows(B * n, 4 + 2 * H, D, torch.float16, 16).to(DEV)
+    k, v, q = qkv[:, 4:6], qkv[:, 6:], qkv[:, :4]
+    batch = binding.FP4Batch(ints([n, n]), n, table_pages=1)
+    got = []
+    for python in (False, True):
+        cache = binding.FP4KVCache(B, H, 4, D)
+        if python:
+            cache._calls = binding._PythonCalls()
+        cache.kv_fp4_append(k, v, batch)
+        kr, vr = cache.kv_fp4_read(batch, B * n, torch.bfloat16)
+        cache.kv_fp4_append(k.unflatten(0, (B, n)), v.unflatten(0, (B, n)), batch)
+        out = cache.kv_fp4_attention(q, batch, 0.1, window=4, sinks=1)
+        assert torch.equal(cache.kv_fp4_attention(q.unflatten(0, (B, n)), batch, 0.1, 4, 1).flatten(0, 1), out)
+        assert torch.equal(cache.kv_fp4_attention(q, batch, 0.1, 4, 1, stream=torch.cuda.current_stream().cuda_stream), out)
+        got.append((kr, vr, out))
+        with pytest.raises(binding.PackKVError):
+            cache.kv_fp4_attention(q, batch, float("nan"))
+        with pytest.raises(binding.PackKVError):
+            cache.kv_fp4_attention(q, batch, 0.1, window=-1)
+        with pytest.raises(binding.PackKVError):
+            cache.kv_fp4_append(k[:, :1].expand(-1, 2, -1), v, batch)
+        cache.close()
+        with pytest.raises(binding.PackKVError):
+            cache.kv_fp4_read(batch, B * n)
+    assert all(torch.equal(a, b) for a, b in zip(*got)) and got[0][2].dtype == torch.float16
