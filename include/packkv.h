@@ -428,8 +428,9 @@ typedef struct {
 int kv_fp4_query_sizes(const kv_fp4_config_t *cfg, kv_fp4_sizes_t *out);
 /*
  * A cache over caller-owned device buffers, both 256-byte aligned and at least as
- * large as kv_fp4_query_sizes said; valid until kv_fp4_cache_destroy.  Host
- * bookkeeping only: the pages' contents are taken as they are (pages that another
+ * large as kv_fp4_query_sizes said; valid until kv_fp4_cache_destroy.  Enqueues a
+ * small kernel on the default stream that clears counters in the workspace and
+ * synchronizes with it.  The pages' contents are taken as they are (pages that another
  * cache of the same configuration has filled can be used).
  */
 int kv_fp4_cache_create(const kv_fp4_config_t *cfg, void *pages, void *workspace, const kv_fp4_sizes_t *sizes,

@@ -487,8 +487,10 @@ class FP4KVCache:
         self.workspace = torch.empty(sizes.workspace, dtype=torch.uint8, device=self.device)
         self.device = self.pages.device
         handle = C.c_void_p()
-        _check(lib().kv_fp4_cache_create(C.byref(self.cfg), self.pages.data_ptr(), self.workspace.data_ptr(),
-                                         C.byref(sizes), C.byref(handle)), "kv_fp4_cache_create")
+        with torch.cuda.device(self.device):
+            torch.cuda.synchronize()
+            _check(lib().kv_fp4_cache_create(C.byref(self.cfg), self.pages.data_ptr(), self.workspace.data_ptr(),
+                                             C.byref(sizes), C.byref(handle)), "kv_fp4_cache_create")
         self._calls = _native.FP4Calls(n_kv_heads, n_q_heads, head_dim, str(self.device)) if _native else _PythonCalls()
         self.handle = handle
         self._calls.set_handle(handle.value)

@@ -47,16 +47,21 @@ struct Fp4Sequence {
     const int32_t *table;
     int64_t base;            // number of page 0 where there is no table
 
-    __device__ inline Fp4Sequence(const Fp4View &v, int b) {
+    // of lens[b], new_rows[b] and first_row[b] as they stand (or would: see raw_rows and raw_first)
+    __device__ inline Fp4Sequence(const Fp4View &v, int b, int raw_len, int raw_rows, int raw_first) {
         const kv_fp4_batch_t &t = v.batch;
-        len = max(t.lens[b], 0);
-        n = t.new_rows ? min(max(t.new_rows[b], 0), t.max_new) : t.max_new;
+        len = max(raw_len, 0);
+        n = t.new_rows ? min(max(raw_rows, 0), t.max_new) : t.max_new;
         pos0 = len - n;
         held = int(min(int64_t(len), int64_t(t.table_pages) * FP4_PAGE));
         base = int64_t(b) * t.table_pages;
         table = t.page_table ? t.page_table + base : nullptr;
-        first = t.first_row ? int64_t(t.first_row[b]) : int64_t(b) * t.max_new;
+        first = t.first_row ? int64_t(raw_first) : int64_t(b) * t.max_new;
     }
+    __device__ inline Fp4Sequence(const Fp4View &v, int b)
+        : Fp4Sequence(v, b, v.batch.lens[b], raw_rows(v, b), raw_first(v, b)) {}
+    static __device__ inline int raw_rows(const Fp4View &v, int b) { return v.batch.new_rows ? v.batch.new_rows[b] : 0; }
+    static __device__ inline int raw_first(const Fp4View &v, int b) { return v.batch.first_row ? v.batch.first_row[b] : 0; }
     // Number of page i < table_pages, or -1 where it is missing.
     __device__ inline int64_t page(const Fp4View &v, int i) const {
         const int64_t p = table ? int64_t(table[i]) : base + i;
@@ -70,5 +75,6 @@ int launch_fp4_read(const kv_fp4_cache *c, const Fp4View &v, void *k, void *vv, 
 int launch_fp4_attention(const kv_fp4_cache *c, const Fp4View &v, const void *q, int64_t q_stride, bool bf16, float sm_scale,
                          int window, int sinks, void *out, int out_type, float *lse, hipStream_t s);
 size_t fp4_workspace_bytes(int head_dim);
+int launch_fp4_clear(const kv_fp4_cache *c, hipStream_t s);   // the workspace's counters, once
 
 }  // namespace packkv

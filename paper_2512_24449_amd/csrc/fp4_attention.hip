@@ -11,7 +11,7 @@
 #include <algorithm>
 
 #include "fp4.h"
-#include "unpack.h"
+#include "last_group.h"
 
 namespace packkv {
 
@@ -28,11 +28,19 @@ constexpr int FP4_COLUMNS = 16;
 // scale no sums then.  They are held as 2^P_LIFT times their size, so that the largest is between 2^12 and 2^15, and fp16
 // keeps its eleven bits down to 2^-26 of it.
 constexpr float P_LIFT = 12.0f, P_SLACK = 3.0f;
-// Partial results: at most so many rows (of a column in a split) of HD + 4 floats.
+// The workspace: a counter byte for each of so many (stream, sequence) pairs whose splits are joined by the last workgroup
+// of them, and partial results, at most so many rows (of a column in a split) of HD + 4 floats.
+constexpr int FP4_COUNTERS = 4096;
 constexpr int64_t FP4_PART_ROWS = 32768;
 constexpr int FP4_SPLITS_MAX = 256;
+// Sequences that share workgroups by their lengths.
+constexpr int FP4_FLAT = 64;
+// Steps that a split has at least: two to a wave in a call of few workgroups, else three.  Passes with two and with three: one
+// head x 1000 tokens 7.8 / 8.5 us, 32 heads x 4100 14.8 / 13.2, a window of 4096 of 8 kv-heads 10.0 / 9.6.
+constexpr int FP4_LEAST_STEPS = 8, FP4_MORE_STEPS = 12;
+constexpr int64_t FP4_FEW_GROUPS = 128;
 
-size_t fp4_workspace_bytes(int head_dim) { return size_t(FP4_PART_ROWS) * (head_dim + 4) * sizeof(float); }
+size_t fp4_workspace_bytes(int head_dim) { return FP4_COUNTERS + size_t(FP4_PART_ROWS) * (head_dim + 4) * sizeof(float); }
 
 struct Fp4Attention {
     Fp4View v;
@@ -43,11 +51,17 @@ struct Fp4Attention {
     void *out;
     int out_type;
     float *lse;
-    float *part;             // partial results, HD sums, maximum and sum of weights each; null: one split
-    int splits, blocks;      // splits of the context, column blocks
+    float *part;             // partial results: HD sums, maximum and sum of the weights
+    uint8_t *counters;       // not null: the last workgroup of a sequence joins its splits
+    int blocks;              // column blocks; a stream is one of them of a kv-head
+    int rows;                // columns of a block with partial results: all, or what max_new has
+    int least_steps;         // of a split (flat)
+    bool flat;               // the workgroups of 64 sequences of a stream go to them by their lengths; else each has as many
+    int splits;              // workgroups of those; or of a stream and sequence
 
-    __device__ inline int64_t part_row(int b, uint32_t stream, int split, int column) const {
-        return ((int64_t(b) * blocks * v.H + stream) * splits + split) * FP4_COLUMNS + column;
+    __device__ inline int64_t part_row(uint32_t stream, int b, int first, int column) const {   // of the first split
+        const int64_t streams = int64_t(blocks) * v.H, at = flat ? (b / FP4_FLAT * streams + stream) * splits + first : (b * streams + stream) * splits;
+        return at * rows + column;
     }
 };
 
@@ -122,6 +136,11 @@ __device__ inline float max3(float a, float b, float c) {   // (without the inst
 // exp2(a - b) where -inf - -inf means no weight.
 __device__ inline float weight_of(float a, float b) { return b == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(a - b); }
 
+// The natural logarithm of a sum of weights l (2^P_LIFT times their size) relative to the maximum m.
+__device__ inline float log_sum(float m, float l) {
+    return l > 0.0f || l != l ? (m - P_LIFT + __log2f(l)) * 0.6931471805599453f : -INFINITY;
+}
+
 template <int N>
 __device__ inline void store_out(void *out, int type, int64_t at, const float (&x)[N]) {
     if (type == KV_TYPE_FP32) {
@@ -147,14 +166,15 @@ struct Fp4Steps {
     int end;                   // tokens from here on are seen by none
     int begin;                 // nor are those below, but for the first ones
     int sink_steps, window_step, n;
-    __device__ inline Fp4Steps(const Fp4Sequence &seq, int column0, int columns, int G, int window, int sinks) {
+    __device__ inline Fp4Steps(const Fp4Sequence &seq, int column0, int G, int window, int sinks) {
+        const int pos0 = seq.pos0, rows = seq.n;
         first_row = column0 / G;
-        last_row = min((column0 + columns - 1) / G, seq.n - 1);
-        end = min(seq.pos0 + last_row + 1, seq.held);
-        begin = window ? max(max(seq.pos0 + first_row, 0) - window + 1, 0) : 0;
+        last_row = min((column0 + FP4_COLUMNS - 1) / G, rows - 1);
+        end = min(pos0 + last_row + 1, seq.held);
+        begin = window ? max(max(pos0 + first_row, 0) - window + 1, 0) : 0;
         window_step = begin / FP4_STEP;
         sink_steps = min((min(window ? sinks : 0, max(end, 0)) + FP4_STEP - 1) / FP4_STEP, window_step);
-        n = end > 0 ? sink_steps + max((end + FP4_STEP - 1) / FP4_STEP - window_step, 0) : 0;
+        n = end > 0 && first_row < rows ? sink_steps + max((end + FP4_STEP - 1) / FP4_STEP - window_step, 0) : 0;
     }
     __device__ inline int token(int step) const { return FP4_STEP * (step < sink_steps ? step : step - sink_steps + window_step); }
 };
@@ -285,6 +305,54 @@ struct Fp4Pages {
     __device__ inline int at(int i) const { return __builtin_amdgcn_readlane(page, i); }
 };
 
+// Which sequence a workgroup works for, and which of how many splits of its steps.  Flat: the workgroups of 64 sequences of
+// a stream are shared out so that none has more steps than some U >= all steps / (workgroups - sequences): the sum of
+// ceil(steps / U) is then at most the workgroups, and a long sequence among short ones has more of them.  Every wave finds
+// the shares by itself, a sequence to a lane.
+struct Fp4Share {
+    int b, split, splits;    // splits 0: no work
+    int first;               // flat: the sequence's first workgroup among those of the 64
+    int b0, mine, before;    // the 64 sequences begin at b0; lane i: splits of sequence b0 + i, of those before it
+    int len, rows, row0;     // and what the batch says of it
+
+    __device__ inline void find(const Fp4Attention &a, int chunk, int column0, int lane) {
+        const kv_fp4_batch_t &t = a.v.batch;
+        b0 = FP4_FLAT * chunk;
+        const int here = min(t.batch - b0, FP4_FLAT);
+        uint32_t steps = 0;
+        len = rows = row0 = 0;
+        if (lane < here) {
+            len = t.lens[b0 + lane], rows = Fp4Sequence::raw_rows(a.v, b0 + lane), row0 = Fp4Sequence::raw_first(a.v, b0 + lane);
+            const Fp4Sequence seq(a.v, b0 + lane, len, rows, row0);
+            // (a row that sees nothing is written, too)
+            if (column0 < seq.n * a.v.G) steps = max(Fp4Steps(seq, column0, a.v.G, a.window, a.sinks).n, 1);
+        }
+        const float all = float(uint32_t(__builtin_amdgcn_readlane(wave_inclusive_scan(int(steps)), 63)));   // at most 64 * 2^25
+        // quotients in fp32: U is too large rather than too small, the splits are then exact
+        const uint32_t most = max(uint32_t(all * __builtin_amdgcn_rcpf(float(a.splits - here)) * (1.0f + 0x1p-20f)) + 1, uint32_t(a.least_steps));
+        uint32_t q = uint32_t(float(steps) * __builtin_amdgcn_rcpf(float(most)));      // at most 2^8: off by one at most
+        q = q * most < steps ? q + 1 : q;
+        mine = int(q * most < steps ? q + 1 : q);
+        before = wave_inclusive_scan(mine) - mine;
+    }
+    __device__ inline void of_sequence(int sequence) {
+        b = sequence;
+        splits = __builtin_amdgcn_readlane(mine, b - b0);
+        first = __builtin_amdgcn_readlane(before, b - b0);
+    }
+    __device__ inline void of_group(int group) {
+        const uint64_t has = __ballot(before <= group && group < before + mine);
+        splits = 0;
+        if (!has) return;
+        of_sequence(b0 + __builtin_ctzll(has));
+        split = group - first;
+    }
+    __device__ inline Fp4Sequence sequence(const Fp4View &v) const {
+        return Fp4Sequence(v, b, __builtin_amdgcn_readlane(len, b - b0), __builtin_amdgcn_readlane(rows, b - b0),
+                           __builtin_amdgcn_readlane(row0, b - b0));
+    }
+};
+
 template <int HD, bool BF16>
 __global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(Fp4Attention a) {
     using P = Fp4Block<HD>;
@@ -293,16 +361,26 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(F
     __shared__ float lds_m[4][FP4_COLUMNS], lds_l[4][FP4_COLUMNS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c16 = lane & 15, g = lane >> 4;
     const Fp4View &v = a.v;
-    const uint32_t stream = blockIdx.x / uint32_t(a.splits);   // (block of columns, kv-head)
-    const int split = int(blockIdx.x - stream * a.splits), b = blockIdx.y;
-    const int block = int(stream / uint32_t(v.H)), h = int(stream - block * v.H);
-    const Fp4Sequence seq(v, b);
-    const int column0 = block * FP4_COLUMNS, columns = seq.n * v.G;
+    __shared__ uint32_t lds_last;
+    const int h = blockIdx.x, block = int(blockIdx.y), column0 = block * FP4_COLUMNS;
+    const uint32_t stream = uint32_t(block) * v.H + h;
+    Fp4Share share;
+    // (numbers of workgroups are the slowest axis: those without work come last and leave no compute unit out)
+    const int chunk = int(blockIdx.z / uint32_t(a.splits)), group = int(blockIdx.z % uint32_t(a.splits));
+    if (a.flat) {
+        share.find(a, chunk, column0, lane);
+        share.of_group(group);
+        if (share.splits == 0) return;
+    } else {
+        share.b = chunk, share.split = group, share.splits = a.splits, share.first = 0;
+    }
+    const Fp4Sequence seq = a.flat ? share.sequence(v) : Fp4Sequence(v, share.b);
+    const int columns = seq.n * v.G;
     if (column0 >= columns) return;
-    const Fp4Steps steps(seq, column0, FP4_COLUMNS, v.G, a.window, a.sinks);
-    const int per_split = (steps.n + a.splits - 1) / a.splits;
-    const int step_end = min((split + 1) * per_split, steps.n);
-    int step = __builtin_amdgcn_readfirstlane(split * per_split + wave);
+    const Fp4Steps steps(seq, column0, v.G, a.window, a.sinks);
+    const int per_split = (steps.n + share.splits - 1) / share.splits;
+    const int step_end = min((share.split + 1) * per_split, steps.n);
+    int step = __builtin_amdgcn_readfirstlane(share.split * per_split + wave);
 
     // this lane's column
     const int column = column0 + c16, row = column / v.G, head = h * v.G + column % v.G;
@@ -375,30 +453,94 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(F
     float to_l = 0.0f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) to_l += lds_l[w][to] * weight_of(lds_m[w][to], to_m);
-    const int to_row = to_column / v.G;
-    const int64_t to_out = seq.first + to_row;
-    if (to_column >= columns || to_out < 0 || to_out >= v.n_rows) return;
-    const int64_t index = to_out * (int64_t(v.H) * v.G) + h * v.G + to_column % v.G;
-    float *rows = a.part ? a.part + a.part_row(b, stream, split, to) * (HD + 4) : nullptr;
-    const float inverse = to_l > 0.0f || to_l != to_l ? 1.0f / to_l : 0.0f;
+    const auto place = [&](int column, int64_t &index) {   // of a column's output row; false: it has none
+        const int64_t out = seq.first + column / v.G;
+        index = out * (int64_t(v.H) * v.G) + h * v.G + column % v.G;
+        return column < columns && out >= 0 && out < v.n_rows;
+    };
+    int64_t index;
+    if (place(to_column, index)) {
+        float *row = a.part + (a.part_row(stream, share.b, share.first, to) + int64_t(share.split) * a.rows) * (HD + 4);
+        const float inverse = to_l > 0.0f || to_l != to_l ? 1.0f / to_l : 0.0f;
 #pragma unroll
-    for (int x = 0; x < VH; ++x) {
-        const int channel = 64 * x + 4 * part;
-        float r[4];
+        for (int x = 0; x < VH; ++x) {
+            const int channel = 64 * x + 4 * part;
+            float r[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            r[i] = (lds_o[0][to][channel + i] + lds_o[1][to][channel + i]) + (lds_o[2][to][channel + i] + lds_o[3][to][channel + i]);
-        if (rows) {
-            *reinterpret_cast<float4 *>(rows + channel) = make_float4(r[0], r[1], r[2], r[3]);
-        } else {
+            for (int i = 0; i < 4; ++i)
+                r[i] = (lds_o[0][to][channel + i] + lds_o[1][to][channel + i]) + (lds_o[2][to][channel + i] + lds_o[3][to][channel + i]);
+            if (share.splits == 1) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) r[i] *= inverse;
-            store_out(a.out, a.out_type, index * HD + channel, r);
+                for (int i = 0; i < 4; ++i) r[i] *= inverse;
+                store_out(a.out, a.out_type, index * HD + channel, r);
+            } else if (a.counters) {
+                store_shared(row + channel, r[0], r[1]);
+                store_shared(row + channel + 2, r[2], r[3]);
+            } else {
+                *reinterpret_cast<float4 *>(row + channel) = make_float4(r[0], r[1], r[2], r[3]);
+            }
+        }
+        if (part == 0) {
+            if (share.splits == 1) {
+                if (a.lse) a.lse[index] = log_sum(to_m, to_l);
+            } else if (a.counters) {
+                store_shared(row + HD, to_m, to_l);
+            } else {
+                row[HD] = to_m, row[HD + 1] = to_l;
+            }
         }
     }
-    if (part == 0) {
-        if (rows) rows[HD] = to_m, rows[HD + 1] = to_l;
-        else if (a.lse) a.lse[index] = to_l > 0.0f || to_l != to_l ? (to_m - P_LIFT + __log2f(to_l)) * 0.6931471805599453f : -INFINITY;
+    if (!a.counters || share.splits == 1) return;
+    if (!last_group(a.counters + stream * v.batch.batch + share.b, share.splits, &lds_last)) return;
+    // HD / 4 threads to a row, four channels each; the other threads take other columns, or other splits of the same where
+    // there are few columns, four rows at a time
+    constexpr int PARTS = 256 / (HD / 4);
+    const int here = min(columns - column0, FP4_COLUMNS), four = threadIdx.x % (HD / 4), team = threadIdx.x / (HD / 4);
+    const int each = here > PARTS / 2 ? 1 : here > PARTS / 4 ? 2 : here > PARTS / 8 ? 4 : PARTS > 8 && here == 1 ? 16 : 8;   // teams to a column
+    const int beside = team % each;
+    for (int c0 = 0; c0 < here; c0 += PARTS / each) {
+        const int c = c0 + team / each;
+        const float *rows = a.part + a.part_row(stream, share.b, share.first, min(c, here - 1)) * (HD + 4);
+        const int64_t pitch = int64_t(a.rows) * (HD + 4);
+        float m = -INFINITY, l = 0.0f, r[4] = {0, 0, 0, 0};
+        for (int s0 = beside; s0 < share.splits; s0 += 4 * each) {
+            float2 x[4], y[4], ml[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float *from = rows + min(s0 + i * each, share.splits - 1) * pitch;
+                x[i] = load_shared(from + 4 * four), y[i] = load_shared(from + 4 * four + 2), ml[i] = load_shared(from + HD);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (s0 + i * each >= share.splits) break;
+                const float now = fmaxf(m, ml[i].x), old = weight_of(m, now), f = weight_of(ml[i].x, now);
+                m = now;
+                l = l * old + ml[i].y * f;
+                r[0] = r[0] * old + x[i].x * f, r[1] = r[1] * old + x[i].y * f;
+                r[2] = r[2] * old + y[i].x * f, r[3] = r[3] * old + y[i].y * f;
+            }
+        }
+        if (each > 1) {      // the teams of a column: one after the other through LDS (here fits in one turn then)
+            float *mine = &lds_o[0][0][0] + team * (HD + 4);
+            *reinterpret_cast<float4 *>(mine + 4 * four) = make_float4(r[0], r[1], r[2], r[3]);
+            if (four == 0) mine[HD] = m, mine[HD + 1] = l;
+            __syncthreads();
+            if (beside) return;
+            for (int i = 1; i < each; ++i) {
+                const float *from = mine + i * (HD + 4);
+                const float4 x = *reinterpret_cast<const float4 *>(from + 4 * four);
+                const float now = fmaxf(m, from[HD]), old = weight_of(m, now), f = weight_of(from[HD], now);
+                m = now;
+                l = l * old + from[HD + 1] * f;
+                r[0] = r[0] * old + x.x * f, r[1] = r[1] * old + x.y * f, r[2] = r[2] * old + x.z * f, r[3] = r[3] * old + x.w * f;
+            }
+        }
+        if (c >= here || !place(column0 + c, index)) continue;
+        const float inverse = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] *= inverse;
+        store_out(a.out, a.out_type, index * HD + 4 * four, r);
+        if (a.lse && four == 0) a.lse[index] = log_sum(m, l);
     }
 }
 
@@ -410,15 +552,22 @@ __global__ __launch_bounds__(256) void fp4_join_kernel(Fp4Attention a) {
     __shared__ float weight[FP4_SPLITS_MAX], sums[PARTS][HD + 4], shared[4];
     const Fp4View &v = a.v;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int column = int(blockIdx.x / uint32_t(v.H)), h = int(blockIdx.x - column * v.H), b = blockIdx.y;
-    const Fp4Sequence seq(v, b);
+    const int column = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+    Fp4Share share;
+    share.splits = a.splits, share.first = 0;
+    if (a.flat) {
+        share.find(a, b / FP4_FLAT, column / FP4_COLUMNS * FP4_COLUMNS, lane);
+        share.of_sequence(b);
+    }
+    const int splits = share.splits;
+    const Fp4Sequence seq = a.flat ? share.sequence(v) : Fp4Sequence(v, b);
     const int64_t out_row = seq.first + column / v.G;
-    if (column >= seq.n * v.G || out_row < 0 || out_row >= v.n_rows) return;
-    const float *rows = a.part + a.part_row(b, column / FP4_COLUMNS * v.H + h, 0, column % FP4_COLUMNS) * (HD + 4);
-    const int64_t pitch = FP4_COLUMNS * (HD + 4);
+    if (splits <= 1 || column >= seq.n * v.G || out_row < 0 || out_row >= v.n_rows) return;
+    const float *rows = a.part + a.part_row(column / FP4_COLUMNS * v.H + h, b, share.first, column % FP4_COLUMNS) * (HD + 4);
+    const int64_t pitch = int64_t(a.rows) * (HD + 4);
     const int s = threadIdx.x;
     static_assert(FP4_SPLITS_MAX <= 256, "a thread to a split");
-    const float my_m = s < a.splits ? rows[s * pitch + HD] : -INFINITY, my_l = s < a.splits ? rows[s * pitch + HD + 1] : 0.0f;
+    const float my_m = s < splits ? rows[s * pitch + HD] : -INFINITY, my_l = s < splits ? rows[s * pitch + HD + 1] : 0.0f;
     const int part = threadIdx.x / (HD / 4), four = threadIdx.x % (HD / 4);
     float m = my_m;
 #pragma unroll
@@ -435,7 +584,7 @@ __global__ __launch_bounds__(256) void fp4_join_kernel(Fp4Attention a) {
     if (lane == 0) shared[wave] = l;
     float4 acc = make_float4(0, 0, 0, 0);
 #pragma unroll 4
-    for (int i = part; i < a.splits; i += PARTS) {
+    for (int i = part; i < splits; i += PARTS) {
         const float4 x = *reinterpret_cast<const float4 *>(rows + i * pitch + 4 * four);
         const float w = weight[i];
         acc.x = fmaf(w, x.x, acc.x), acc.y = fmaf(w, x.y, acc.y), acc.z = fmaf(w, x.z, acc.z), acc.w = fmaf(w, x.w, acc.w);
@@ -454,8 +603,27 @@ __global__ __launch_bounds__(256) void fp4_join_kernel(Fp4Attention a) {
     if (a.out_type == KV_TYPE_FP32) static_cast<float *>(a.out)[at] = r;
     else if (a.out_type == KV_TYPE_BF16) static_cast<__bf16 *>(a.out)[at] = __bf16(r);
     else static_cast<_Float16 *>(a.out)[at] = _Float16(r);
-    if (a.lse && threadIdx.x == 0) a.lse[index] = some ? (m - P_LIFT + __log2f(l)) * 0.6931471805599453f : -INFINITY;
+    if (a.lse && threadIdx.x == 0) a.lse[index] = log_sum(m, l);
 }
+
+__global__ __launch_bounds__(64) void fp4_clear_kernel(uint32_t *counters) {
+    for (int i = threadIdx.x; i < int(FP4_COUNTERS / sizeof(uint32_t)); i += 64) counters[i] = 0;
+}
+
+int launch_fp4_clear(const kv_fp4_cache *c, hipStream_t s) {
+    hipLaunchKernelGGL(fp4_clear_kernel, dim3(1), dim3(64), 0, s, reinterpret_cast<uint32_t *>(c->workspace));
+    KV_HIP_CHECK(hipGetLastError());
+    return KV_OK;
+}
+
+// Workgroups that a call is split into at most: not quite two to each of the 256 compute units (a third one on some of them
+// would hold up the call).  Four sequences of up to 32788 tokens, 8 kv-heads: 480 workgroups 26.9 us, 512 28.3, 256 27.1, 768 29.
+constexpr int64_t FP4_GROUPS = 480;
+// The last workgroup of a sequence joins its splits itself up to so many rows of partial results; beyond, a kernel with a
+// workgroup to each row of the output does.  Passes joined so / by the kernel: one head x 1000 tokens 7.8 / 8.6 us, a window
+// of 4096 of 8 kv-heads in 11 splits 9.6 / 10.6, four sequences of up to 32788 28.3 / 29, 32 heads x 4100 in 11 splits 13.2 /
+// 13.0; where no sequence turns out to be split (8 sequences x 52 heads) the kernel would be launched for nothing.
+constexpr int64_t FP4_MERGED_ROWS = 256;
 
 int launch_fp4_attention(const kv_fp4_cache *c, const Fp4View &v, const void *q, int64_t q_stride, bool bf16, float sm_scale,
                          int window, int sinks, void *out, int out_type, float *lse, hipStream_t s) {
@@ -469,16 +637,27 @@ int launch_fp4_attention(const kv_fp4_cache *c, const Fp4View &v, const void *q,
     a.window = window, a.sinks = sinks;
     a.out = out, a.out_type = out_type, a.lse = lse;
     a.blocks = int((columns + FP4_COLUMNS - 1) / FP4_COLUMNS);
-    const int64_t streams = int64_t(a.blocks) * v.batch.batch * v.H;
+    a.rows = int(std::min<int64_t>(columns, FP4_COLUMNS));
     // Steps that a block of columns can have.
     int64_t most = int64_t(v.batch.table_pages) * (FP4_PAGE / FP4_STEP);
     if (window) most = std::min(most, (int64_t(window) + FP4_COLUMNS + sinks) / FP4_STEP + 3);
-    int64_t splits = std::min<int64_t>({1024 / streams, (most + 7) / 8, FP4_SPLITS_MAX, FP4_PART_ROWS / FP4_COLUMNS / streams});
-    a.splits = int(std::max<int64_t>(splits, 1));
-    a.part = a.splits > 1 ? c->workspace : nullptr;
-    const int64_t groups = int64_t(a.blocks) * v.H * a.splits;
-    if (groups > 0x7FFFFFFF || columns * v.H > 0x7FFFFFFF) return KV_ERR_UNSUPPORTED;
-    const dim3 grid(unsigned(groups), unsigned(v.batch.batch));
+    const int batch = v.batch.batch;
+    const int64_t streams = int64_t(a.blocks) * v.H, room = FP4_PART_ROWS / a.rows / streams;   // workgroups that the workspace takes
+    a.least_steps = streams * batch * (most / FP4_LEAST_STEPS) <= FP4_FEW_GROUPS ? FP4_LEAST_STEPS : FP4_MORE_STEPS;
+    const int64_t useful = (most + a.least_steps - 1) / a.least_steps;       // splits of a sequence
+    const int chunk = std::min(batch, FP4_FLAT), chunks = (batch + FP4_FLAT - 1) / FP4_FLAT;
+    int64_t want = FP4_GROUPS / streams;
+    a.flat = batch > 1 && useful > 1 && room >= 2 * chunk * chunks;
+    if (a.flat)
+        a.splits = int(std::min({std::max<int64_t>(want / chunks, 2 * chunk), chunk * (1 + useful), room / chunks, int64_t(FP4_SPLITS_MAX)}));
+    else
+        a.splits = int(std::max<int64_t>(std::min({want / batch, useful, room / batch, int64_t(FP4_SPLITS_MAX)}), 1));
+    const int64_t groups = int64_t(a.flat ? chunks : batch) * a.splits;
+    if (a.blocks > 65535 || groups > 65535) return KV_ERR_UNSUPPORTED;
+    const bool merged = a.splits > 1 && a.splits <= 64 && streams * batch <= FP4_COUNTERS && a.rows * a.splits <= FP4_MERGED_ROWS;
+    a.counters = merged ? reinterpret_cast<uint8_t *>(c->workspace) : nullptr;
+    a.part = c->workspace + FP4_COUNTERS / sizeof(float);
+    const dim3 grid = dim3(uint32_t(v.H), uint32_t(a.blocks), uint32_t(groups));
 #define LAUNCH(HD, BF) hipLaunchKernelGGL((fp4_attention_kernel<HD, BF>), grid, dim3(256), 0, s, a)
     if (c->cfg.head_dim == 128) {
         if (bf16) LAUNCH(128, true); else LAUNCH(128, false);
@@ -487,8 +666,8 @@ int launch_fp4_attention(const kv_fp4_cache *c, const Fp4View &v, const void *q,
     }
 #undef LAUNCH
     KV_HIP_CHECK(hipGetLastError());
-    if (a.splits > 1) {
-        const dim3 grid(unsigned(columns * v.H), unsigned(v.batch.batch));
+    if (a.splits > 1 && !a.counters) {
+        const dim3 grid = dim3(uint32_t(columns), uint32_t(v.H), uint32_t(batch));
         if (c->cfg.head_dim == 128) hipLaunchKernelGGL(fp4_join_kernel<128>, grid, dim3(256), 0, s, a);
         else hipLaunchKernelGGL(fp4_join_kernel<64>, grid, dim3(256), 0, s, a);
         KV_HIP_CHECK(hipGetLastError());

@@ -248,7 +248,7 @@ int launch_fp4_append(const kv_fp4_cache *c, const Fp4View &v, const void *k, in
     const int tiles = tiles_touched(v.batch.max_new, c->cfg.head_dim == 128 ? Fp4Tile<128>::TOKENS : Fp4Tile<64>::TOKENS);
     const int64_t groups = (int64_t(tiles) * v.H + 3) / 4;
     if (groups > 0x1FFFFFFF) return KV_ERR_UNSUPPORTED;
-    const dim3 grid(unsigned(groups), unsigned(v.batch.batch));
+    const dim3 grid = dim3(uint32_t(groups), uint32_t(v.batch.batch));
 #define LAUNCH(HD, BF)                                                                                                    \
     hipLaunchKernelGGL((fp4_append_kernel<HD, BF>), grid, dim3(256), 0, s, v, static_cast<const uint16_t *>(k), \
                        k_stride, static_cast<const uint16_t *>(vv), v_stride, tiles)
@@ -266,7 +266,7 @@ int launch_fp4_read(const kv_fp4_cache *c, const Fp4View &v, void *k, void *vv, 
     const int tiles = tiles_touched(v.batch.max_new, c->cfg.head_dim == 128 ? Fp4Tile<128>::TOKENS : Fp4Tile<64>::TOKENS);
     const int64_t groups = (int64_t(tiles) * v.H + 3) / 4;
     if (groups > 0x1FFFFFFF) return KV_ERR_UNSUPPORTED;
-    const dim3 grid(unsigned(groups), unsigned(v.batch.batch));
+    const dim3 grid = dim3(uint32_t(groups), uint32_t(v.batch.batch));
 #define LAUNCH(HD, TYPE)                                                                                                  \
     hipLaunchKernelGGL((fp4_read_kernel<HD, TYPE>), grid, dim3(256), 0, s, v, static_cast<uint8_t *>(k), \
                        static_cast<uint8_t *>(vv), tiles)
@@ -341,6 +341,12 @@ extern "C" int kv_fp4_cache_create(const kv_fp4_config_t *cfg, void *pages, void
     c->cfg = *cfg;
     c->pages = static_cast<uint8_t *>(pages);
     c->workspace = static_cast<float *>(workspace);
+    int made = launch_fp4_clear(c, nullptr);
+    if (made == KV_OK && hipStreamSynchronize(nullptr) != hipSuccess) made = KV_ERR_HIP;
+    if (made) {
+        delete c;
+        return made;
+    }
     *out = c;
     return KV_OK;
 }

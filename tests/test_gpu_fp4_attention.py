@@ -254,3 +254,18 @@ def test_pages_behind_4_gib():
     lse = torch.empty(70, H, device=DEV)
     out = cache.kv_fp4_attention(q, batch, 0.1, lse=lse)
     check(cache, ref.quantise(k.cpu())[0], ref.quantise(v.cpu())[0], [70], [70], q, out, lse, 0.1)
+
+
+@pytest.mark.parametrize("H, G, lens", [(2, 1, [9000] + [5] * 20), (1, 4, [40, 6000, 41]), (2, 2, [100] * 70 + [3000] + [1] * 5),
+                                        (1, 16, [7000, 0, 900]), (1, 1, [130] * 129)])
+def test_very_different_lengths(H, G, lens):
+    """A long sequence among short ones is split over more workgroups; more sequences than one wave shares out."""
+    run(lens, [1] * len(lens), H, G, 64, torch.float16, seed=len(lens))
+    run(lens, [min(n, 2) for n in lens], H, G, 64, torch.bfloat16, 50, 3, seed=len(lens))
+
+
+@pytest.mark.parametrize("G", [1, 2, 3, 5, 8, 16])
+def test_joined_by_the_last_workgroup_and_by_a_kernel(G):
+    """Splits of one sequence: few rows (joined where they are made) and many."""
+    for lens in ([1200], [20000]):
+        run(lens, [1], 1, G, 128 if G < 4 else 64, torch.float16, seed=G)
