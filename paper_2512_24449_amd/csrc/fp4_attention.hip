@@ -1,183 +1,10 @@
-// Attention over the 4-bit paged cache, one pass with the running maximum and sum of a softmax.
-//
-// Scores are computed transposed: S^T = K Q^T (rows: tokens, columns: the query heads of a kv-head, of one or several new
-// rows), then O^T = V^T P^T.  A lane then holds scores, weights and outputs of one column only, so maximum and sum are the
-// lane's own (joined over the four lanes of a column), and the layout in which the matrix cores leave S^T is the one in which
-// they take P^T: nothing passes through LDS or other lanes between the two products.  Which 32 tokens a step's rows stand
-// for is free as long as both products agree; row 4g + i of the first (second) product of 16 is token 8g + i (8g + 4 + i), so
-// that a lane's eight weights are eight consecutive tokens: a word of V.
-//
-// K and V enter as fp16 (K as bf16 where q is): E2M1 numbers with scales 2^-23 .. 2^13 are exact there.
-#include <algorithm>
-
-#include "fp4.h"
-#include "last_group.h"
+// Attention over the 4-bit paged cache for few new rows: a wave streams the cache past 16 columns.  Bound by the rate at
+// which HBM delivers pages.
+#include "fp4_attention.h"
 
 namespace packkv {
 
-typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
-typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
-typedef __bf16 bf162_t __attribute__((ext_vector_type(2)));
-typedef __bf16 bf168_t __attribute__((ext_vector_type(8)));
-typedef float float4_t __attribute__((ext_vector_type(4)));
-typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
-
-constexpr int FP4_STEP = 32;             // tokens of a step: half a page
-constexpr int FP4_COLUMNS = 16;
-// Weights are relative to a maximum that follows the scores only when one is P_SLACK (in powers of two) above it: most steps
-// scale no sums then.  They are held as 2^P_LIFT times their size, so that the largest is between 2^12 and 2^15, and fp16
-// keeps its eleven bits down to 2^-26 of it.
-constexpr float P_LIFT = 12.0f, P_SLACK = 3.0f;
-// The workspace: a counter byte for each of so many (stream, sequence) pairs whose splits are joined by the last workgroup
-// of them, and partial results, at most so many rows (of a column in a split) of HD + 4 floats.
-constexpr int FP4_COUNTERS = 4096;
-constexpr int64_t FP4_PART_ROWS = 32768;
-constexpr int FP4_SPLITS_MAX = 256;
-// Sequences that share workgroups by their lengths.
-constexpr int FP4_FLAT = 64;
-// Steps that a split has at least: two to a wave in a call of few workgroups, else three.  Passes with two and with three: one
-// head x 1000 tokens 7.8 / 8.5 us, 32 heads x 4100 14.8 / 13.2, a window of 4096 of 8 kv-heads 10.0 / 9.6.
-constexpr int FP4_LEAST_STEPS = 8, FP4_MORE_STEPS = 12;
-constexpr int64_t FP4_FEW_GROUPS = 128;
-
 size_t fp4_workspace_bytes(int head_dim) { return FP4_COUNTERS + size_t(FP4_PART_ROWS) * (head_dim + 4) * sizeof(float); }
-
-struct Fp4Attention {
-    Fp4View v;
-    const uint16_t *q;
-    int64_t q_stride;
-    float scale;             // sm_scale * log2(e)
-    int window, sinks;
-    void *out;
-    int out_type;
-    float *lse;
-    float *part;             // partial results: HD sums, maximum and sum of the weights
-    uint8_t *counters;       // not null: the last workgroup of a sequence joins its splits
-    int blocks;              // column blocks; a stream is one of them of a kv-head
-    int rows;                // columns of a block with partial results: all, or what max_new has
-    int least_steps;         // of a split (flat)
-    bool flat;               // the workgroups of 64 sequences of a stream go to them by their lengths; else each has as many
-    int splits;              // workgroups of those; or of a stream and sequence
-
-    __device__ inline int64_t part_row(uint32_t stream, int b, int first, int column) const {   // of the first split
-        const int64_t streams = int64_t(blocks) * v.H, at = flat ? (b / FP4_FLAT * streams + stream) * splits + first : (b * streams + stream) * splits;
-        return at * rows + column;
-    }
-};
-
-// Four words of a row (32 values' codes, HD / 4 of a lane) as operands: value pairs in the order of the channels.
-template <bool BF16>
-__device__ inline uint4_t row_operand(uint32_t w, float scale) {
-    if constexpr (BF16)
-        return uint4_t{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
-                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
-                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)),
-                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3))};
-    else
-        return uint4_t{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0)),
-                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1)),
-                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2)),
-                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3))};
-}
-
-template <bool BF16>
-__device__ inline float4_t product16(uint4_t a, uint4_t b, float4_t c) {
-    if constexpr (BF16)
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf168_t, a), __builtin_bit_cast(bf168_t, b), c, 0, 0, 0);
-    else
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
-}
-
-// The scales of eight tokens (bytes e + 127) as fp16 pairs.
-__device__ inline void scale_pairs(uint2 bytes, half2_t (&out)[4]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t two = (i < 2 ? bytes.x : bytes.y) >> (16 * (i & 1));
-        out[i] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_pkrtz(__uint_as_float((two & 255u) << 23),
-                                                                         __uint_as_float(((two >> 8) & 255u) << 23)));
-    }
-}
-
-// A word of V (one channel of eight tokens) with the tokens' scales.
-__device__ inline uint4_t column_operand(uint32_t w, const half2_t (&scale)[4]) {
-    uint4_t r;
-    r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 0) * scale[0]);
-    r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 1) * scale[1]);
-    r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 2) * scale[2]);
-    r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 3) * scale[3]);
-    return r;
-}
-
-// Maximum and sum over the four lanes of a column (lane, lane ^ 16, lane ^ 32, lane ^ 48).
-__device__ inline float column_max(float x) {
-    uint32_t a = __float_as_uint(x), b = a;
-    swap_rows16(a, b);
-    x = fmaxf(__uint_as_float(a), __uint_as_float(b));
-    a = b = __float_as_uint(x);
-    swap_rows32(a, b);
-    return fmaxf(__uint_as_float(a), __uint_as_float(b));
-}
-
-__device__ inline float column_sum(float x) {
-    uint32_t a = __float_as_uint(x), b = a;
-    swap_rows16(a, b);
-    x = __uint_as_float(a) + __uint_as_float(b);
-    a = b = __float_as_uint(x);
-    swap_rows32(a, b);
-    return __uint_as_float(a) + __uint_as_float(b);
-}
-
-__device__ inline float max3(float a, float b, float c) {   // (without the instructions that quiet a signalling NaN first)
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-    return r;
-}
-
-// exp2(a - b) where -inf - -inf means no weight.
-__device__ inline float weight_of(float a, float b) { return b == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(a - b); }
-
-// The natural logarithm of a sum of weights l (2^P_LIFT times their size) relative to the maximum m.
-__device__ inline float log_sum(float m, float l) {
-    return l > 0.0f || l != l ? (m - P_LIFT + __log2f(l)) * 0.6931471805599453f : -INFINITY;
-}
-
-template <int N>
-__device__ inline void store_out(void *out, int type, int64_t at, const float (&x)[N]) {
-    if (type == KV_TYPE_FP32) {
-#pragma unroll
-        for (int i = 0; i < N; i += 4)
-            *reinterpret_cast<float4 *>(static_cast<float *>(out) + at + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
-        return;
-    }
-    uint32_t w[N / 2];
-#pragma unroll
-    for (int i = 0; i < N; i += 2)
-        w[i / 2] = type == KV_TYPE_BF16 ? __builtin_bit_cast(uint32_t, bf162_t{__bf16(x[i]), __bf16(x[i + 1])})
-                                        : __builtin_bit_cast(uint32_t, half2_t{_Float16(x[i]), _Float16(x[i + 1])});
-#pragma unroll
-    for (int i = 0; i < N / 2; i += 2)
-        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(out) + at + 2 * i) = make_uint2(w[i], w[i + 1]);
-}
-
-// The tokens that a block of columns sees, in steps of 32: those that hold first tokens, then those from the window's
-// start to the last row.
-struct Fp4Steps {
-    int first_row, last_row;   // new rows of the block
-    int end;                   // tokens from here on are seen by none
-    int begin;                 // nor are those below, but for the first ones
-    int sink_steps, window_step, n;
-    __device__ inline Fp4Steps(const Fp4Sequence &seq, int column0, int G, int window, int sinks) {
-        const int pos0 = seq.pos0, rows = seq.n;
-        first_row = column0 / G;
-        last_row = min((column0 + FP4_COLUMNS - 1) / G, rows - 1);
-        end = min(pos0 + last_row + 1, seq.held);
-        begin = window ? max(max(pos0 + first_row, 0) - window + 1, 0) : 0;
-        window_step = begin / FP4_STEP;
-        sink_steps = min((min(window ? sinks : 0, max(end, 0)) + FP4_STEP - 1) / FP4_STEP, window_step);
-        n = end > 0 && first_row < rows ? sink_steps + max((end + FP4_STEP - 1) / FP4_STEP - window_step, 0) : 0;
-    }
-    __device__ inline int token(int step) const { return FP4_STEP * (step < sink_steps ? step : step - sink_steps + window_step); }
-};
 
 // What a wave reads of a step: of K a lane's quarter of two tokens' rows, of V a word (or HD / 64 times four) of eight tokens.
 template <int HD>
@@ -215,86 +42,6 @@ struct Fp4Stage {
     }
 };
 
-// The columns of a wave's matrix products, its running softmax and its sums.
-template <int HD, bool BF16>
-struct Fp4Columns {
-    static constexpr int KW = HD / 32, VH = HD / 64, OT = HD / 16;
-    uint4_t q[KW];
-    float4_t o[OT];
-    float l, m, bar, lift;   // sum of this lane's weights; what the weights are relative to; score that moves it; P_LIFT - m * scale
-    int hi, lo;              // last token that the column sees; first of its window
-    float scale, slack;      // slack: P_SLACK / scale
-    int sinks, begin;
-
-    __device__ inline void clear() {
-#pragma unroll
-        for (int i = 0; i < OT; ++i) o[i] = float4_t{0, 0, 0, 0};
-        l = 0.0f;
-        m = bar = -INFINITY;
-        lift = P_LIFT;
-    }
-
-    // edge (wave-uniform): there are tokens that not every column sees
-    __device__ inline void step(const Fp4Stage<HD> &in, int g, bool edge) {
-        float4_t s[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            s[t] = float4_t{0, 0, 0, 0};
-            const float ks = __uint_as_float(in.ks[t] << 23);
-#pragma unroll
-            for (int i = 0; i < KW; ++i) s[t] = product16<BF16>(row_operand<BF16>(in.k[t][i], ks), q[i], s[t]);
-        }
-        uint2 vs[VH];
-#pragma unroll
-        for (int x = 0; x < VH; ++x) vs[x] = in.vs[x];
-        if (edge) {
-            uint32_t keep[2] = {0, 0};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int t = in.t0 + 8 * g + i;
-                const bool ok = (t <= hi) & (t < in.end) & ((t >= lo) | (t < sinks));
-                s[i >> 2][i & 3] = ok ? s[i >> 2][i & 3] : -INFINITY;
-                // a token that no row sees may be any bits: no infinity times a weight of 0
-                const bool seen = (t < in.end) & ((t >= begin) | (t < sinks));
-                keep[i >> 2] |= seen ? 255u << (8 * (i & 3)) : 0u;
-            }
-#pragma unroll
-            for (int x = 0; x < VH; ++x) vs[x].x &= keep[0], vs[x].y &= keep[1];
-        }
-        float top = max3(max3(s[0][0], s[0][1], s[0][2]), max3(s[0][3], s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]));
-        if (__any(top > bar)) {
-            top = column_max(top);
-            if (top > bar) {
-                const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - top) * scale);
-#pragma unroll
-                for (int i = 0; i < OT; ++i) o[i] *= f;
-                l *= f;
-                m = top;
-                bar = top + slack;
-                lift = P_LIFT - top * scale;
-            }
-        }
-        half2_t p[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float x = __builtin_amdgcn_exp2f(fmaf(s[i >> 1][2 * (i & 1)], scale, lift));
-            const float y = __builtin_amdgcn_exp2f(fmaf(s[i >> 1][2 * (i & 1) + 1], scale, lift));
-            l += x + y;
-            p[i] = half2_t{_Float16(x), _Float16(y)};
-        }
-        const uint4_t pw = {__builtin_bit_cast(uint32_t, p[0]), __builtin_bit_cast(uint32_t, p[1]), __builtin_bit_cast(uint32_t, p[2]),
-                            __builtin_bit_cast(uint32_t, p[3])};
-#pragma unroll
-        for (int x = 0; x < VH; ++x) {
-            half2_t scales[4];
-            scale_pairs(vs[x], scales);
-            const uint32_t words[4] = {in.v[x].x, in.v[x].y, in.v[x].z, in.v[x].w};
-#pragma unroll
-            for (int c = 0; c < 4; ++c) o[4 * x + c] = product16<false>(column_operand(words[c], scales), pw, o[4 * x + c]);
-        }
-    }
-};
-
 // The page numbers of the next 64 steps of a wave, one to a lane: none of its transfers waits for the table.
 struct Fp4Pages {
     int page;                // (page numbers fit 31 bits) -1: missing
@@ -303,54 +50,6 @@ struct Fp4Pages {
         page = mine < end ? int(seq.page(v, steps.token(mine) / FP4_PAGE)) : -1;
     }
     __device__ inline int at(int i) const { return __builtin_amdgcn_readlane(page, i); }
-};
-
-// Which sequence a workgroup works for, and which of how many splits of its steps.  Flat: the workgroups of 64 sequences of
-// a stream are shared out so that none has more steps than some U >= all steps / (workgroups - sequences): the sum of
-// ceil(steps / U) is then at most the workgroups, and a long sequence among short ones has more of them.  Every wave finds
-// the shares by itself, a sequence to a lane.
-struct Fp4Share {
-    int b, split, splits;    // splits 0: no work
-    int first;               // flat: the sequence's first workgroup among those of the 64
-    int b0, mine, before;    // the 64 sequences begin at b0; lane i: splits of sequence b0 + i, of those before it
-    int len, rows, row0;     // and what the batch says of it
-
-    __device__ inline void find(const Fp4Attention &a, int chunk, int column0, int lane) {
-        const kv_fp4_batch_t &t = a.v.batch;
-        b0 = FP4_FLAT * chunk;
-        const int here = min(t.batch - b0, FP4_FLAT);
-        uint32_t steps = 0;
-        len = rows = row0 = 0;
-        if (lane < here) {
-            len = t.lens[b0 + lane], rows = Fp4Sequence::raw_rows(a.v, b0 + lane), row0 = Fp4Sequence::raw_first(a.v, b0 + lane);
-            const Fp4Sequence seq(a.v, b0 + lane, len, rows, row0);
-            // (a row that sees nothing is written, too)
-            if (column0 < seq.n * a.v.G) steps = max(Fp4Steps(seq, column0, a.v.G, a.window, a.sinks).n, 1);
-        }
-        const float all = float(uint32_t(__builtin_amdgcn_readlane(wave_inclusive_scan(int(steps)), 63)));   // at most 64 * 2^25
-        // quotients in fp32: U is too large rather than too small, the splits are then exact
-        const uint32_t most = max(uint32_t(all * __builtin_amdgcn_rcpf(float(a.splits - here)) * (1.0f + 0x1p-20f)) + 1, uint32_t(a.least_steps));
-        uint32_t q = uint32_t(float(steps) * __builtin_amdgcn_rcpf(float(most)));      // at most 2^8: off by one at most
-        q = q * most < steps ? q + 1 : q;
-        mine = int(q * most < steps ? q + 1 : q);
-        before = wave_inclusive_scan(mine) - mine;
-    }
-    __device__ inline void of_sequence(int sequence) {
-        b = sequence;
-        splits = __builtin_amdgcn_readlane(mine, b - b0);
-        first = __builtin_amdgcn_readlane(before, b - b0);
-    }
-    __device__ inline void of_group(int group) {
-        const uint64_t has = __ballot(before <= group && group < before + mine);
-        splits = 0;
-        if (!has) return;
-        of_sequence(b0 + __builtin_ctzll(has));
-        split = group - first;
-    }
-    __device__ inline Fp4Sequence sequence(const Fp4View &v) const {
-        return Fp4Sequence(v, b, __builtin_amdgcn_readlane(len, b - b0), __builtin_amdgcn_readlane(rows, b - b0),
-                           __builtin_amdgcn_readlane(row0, b - b0));
-    }
 };
 
 template <int HD, bool BF16>
@@ -377,7 +76,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(F
     const Fp4Sequence seq = a.flat ? share.sequence(v) : Fp4Sequence(v, share.b);
     const int columns = seq.n * v.G;
     if (column0 >= columns) return;
-    const Fp4Steps steps(seq, column0, v.G, a.window, a.sinks);
+    const Fp4Steps steps(seq, column0, FP4_COLUMNS, v.G, a.window, a.sinks);
     const int per_split = (steps.n + share.splits - 1) / share.splits;
     const int step_end = min((share.split + 1) * per_split, steps.n);
     int step = __builtin_amdgcn_readfirstlane(share.split * per_split + wave);
@@ -386,19 +85,15 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(F
     const int column = column0 + c16, row = column / v.G, head = h * v.G + column % v.G;
     const int64_t out_row = seq.first + row;
     const bool real = column < columns && out_row >= 0 && out_row < v.n_rows;
-    Fp4Columns<HD, BF16> col;
+    Fp4Column<HD> col;
     col.hi = max(seq.pos0 + row, -1), col.lo = a.window ? col.hi - a.window + 1 : 0;
-    col.sinks = a.sinks, col.begin = steps.begin;
-    // A negative scale is one of -q: the largest scaled score is then that of the largest score.  Scores are below 2^39, so
-    // below 1e-30 all that are seen weigh the same, as with 0 (which would make a NaN of a score that is not seen).
-    col.scale = fmaxf(fabsf(a.scale), 1e-30f);
-    const uint32_t sign = a.scale < 0.0f ? 0x80008000u : 0u;
+    const Fp4Scale scale(a.scale);
+    uint4_t q[KW];
 #pragma unroll
     for (int i = 0; i < KW; ++i) {
-        col.q[i] = uint4_t{0, 0, 0, 0};
-        if (real) col.q[i] = *reinterpret_cast<const uint4_t *>(a.q + out_row * a.q_stride + int64_t(head) * HD + g * (HD / 4) + 8 * i) ^ sign;
+        q[i] = uint4_t{0, 0, 0, 0};
+        if (real) q[i] = *reinterpret_cast<const uint4_t *>(a.q + out_row * a.q_stride + int64_t(head) * HD + g * (HD / 4) + 8 * i) ^ scale.sign;
     }
-    col.slack = P_SLACK / col.scale;
     col.clear();
     // a step whose tokens every column of the block sees needs no masks
     const int first_hi = max(seq.pos0 + steps.first_row, -1), last_lo = a.window ? max(seq.pos0 + steps.last_row - a.window + 1, 0) : 0;
@@ -413,7 +108,32 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(F
         to.load(v.pages + (int64_t(max(page, 0)) * v.H + h) * size_t(P::BYTES), to.t0 % FP4_PAGE, c16, g);
     };
     auto compute = [&](const Fp4Stage<HD> &from) {
-        col.step(from, g, from.t0 + FP4_STEP > min(from.end, first_hi + 1) || from.t0 < last_lo);
+        float4_t s[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            s[t] = float4_t{0, 0, 0, 0};
+            const float ks = __uint_as_float(from.ks[t] << 23);
+#pragma unroll
+            for (int i = 0; i < KW; ++i) s[t] = product16<BF16>(row_operand<BF16>(from.k[t][i], ks), q[i], s[t]);
+        }
+        uint2 vs[VH];
+#pragma unroll
+        for (int x = 0; x < VH; ++x) vs[x] = from.vs[x];
+        if (from.t0 + FP4_STEP > min(from.end, first_hi + 1) || from.t0 < last_lo) {   // (wave-uniform)
+            const int t8 = from.t0 + 8 * g;
+            col.mask(s, t8, from.end, a.sinks);
+#pragma unroll
+            for (int x = 0; x < VH; ++x) vs[x] = seen_scales(vs[x], t8, steps.begin, from.end, a.sinks);
+        }
+        const uint4_t p = col.weigh(s, scale);
+#pragma unroll
+        for (int x = 0; x < VH; ++x) {
+            half2_t scales[4];
+            scale_pairs(vs[x], scales);
+            const uint32_t words[4] = {from.v[x].x, from.v[x].y, from.v[x].z, from.v[x].w};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) col.o[4 * x + c] = product16<false>(column_operand(words[c], scales), p, col.o[4 * x + c]);
+        }
     };
     for (; step < step_end; step += 4 * 64) {
         pages.load(v, seq, steps, step, step_end, lane);
@@ -431,7 +151,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(F
         }
     }
     float4_t(&o)[OT] = col.o;
-    const float l = column_sum(col.l), m = col.m == -INFINITY ? col.m : col.m * col.scale;
+    const float l = column_sum(col.l), m = col.scaled_max(scale);
 
     // The four waves' results: each scaled to their common maximum, then summed.  A lane's o[4x + c][i] is channel
     // 64x + 16g + 4i + c.
@@ -556,14 +276,14 @@ __global__ __launch_bounds__(256) void fp4_join_kernel(Fp4Attention a) {
     Fp4Share share;
     share.splits = a.splits, share.first = 0;
     if (a.flat) {
-        share.find(a, b / FP4_FLAT, column / FP4_COLUMNS * FP4_COLUMNS, lane);
+        share.find(a, b / FP4_FLAT, column / a.width * a.width, lane);
         share.of_sequence(b);
     }
     const int splits = share.splits;
     const Fp4Sequence seq = a.flat ? share.sequence(v) : Fp4Sequence(v, b);
     const int64_t out_row = seq.first + column / v.G;
     if (splits <= 1 || column >= seq.n * v.G || out_row < 0 || out_row >= v.n_rows) return;
-    const float *rows = a.part + a.part_row(column / FP4_COLUMNS * v.H + h, b, share.first, column % FP4_COLUMNS) * (HD + 4);
+    const float *rows = a.part + a.part_row(column / a.width * v.H + h, b, share.first, column % a.width) * (HD + 4);
     const int64_t pitch = int64_t(a.rows) * (HD + 4);
     const int s = threadIdx.x;
     static_assert(FP4_SPLITS_MAX <= 256, "a thread to a split");
@@ -616,6 +336,8 @@ int launch_fp4_clear(const kv_fp4_cache *c, hipStream_t s) {
     return KV_OK;
 }
 
+// Columns of a kv-head up to which the streaming kernel takes them (in blocks of 16, each a pass over the cache).
+constexpr int64_t FP4_FEW_COLUMNS = 32;
 // Workgroups that a call is split into at most: not quite two to each of the 256 compute units (a third one on some of them
 // would hold up the call).  Four sequences of up to 32788 tokens, 8 kv-heads: 480 workgroups 26.9 us, 512 28.3, 256 27.1, 768 29.
 constexpr int64_t FP4_GROUPS = 480;
@@ -636,11 +358,12 @@ int launch_fp4_attention(const kv_fp4_cache *c, const Fp4View &v, const void *q,
     a.scale = sm_scale * 1.4426950408889634f;
     a.window = window, a.sinks = sinks;
     a.out = out, a.out_type = out_type, a.lse = lse;
-    a.blocks = int((columns + FP4_COLUMNS - 1) / FP4_COLUMNS);
-    a.rows = int(std::min<int64_t>(columns, FP4_COLUMNS));
+    a.width = columns > FP4_FEW_COLUMNS ? FP4_TILE_COLUMNS : FP4_COLUMNS;
+    a.blocks = int((columns + a.width - 1) / a.width);
+    a.rows = int(std::min<int64_t>(columns, a.width));
     // Steps that a block of columns can have.
     int64_t most = int64_t(v.batch.table_pages) * (FP4_PAGE / FP4_STEP);
-    if (window) most = std::min(most, (int64_t(window) + FP4_COLUMNS + sinks) / FP4_STEP + 3);
+    if (window) most = std::min(most, (int64_t(window) + a.width + sinks) / FP4_STEP + 3);
     const int batch = v.batch.batch;
     const int64_t streams = int64_t(a.blocks) * v.H, room = FP4_PART_ROWS / a.rows / streams;   // workgroups that the workspace takes
     a.least_steps = streams * batch * (most / FP4_LEAST_STEPS) <= FP4_FEW_GROUPS ? FP4_LEAST_STEPS : FP4_MORE_STEPS;
@@ -654,12 +377,15 @@ int launch_fp4_attention(const kv_fp4_cache *c, const Fp4View &v, const void *q,
         a.splits = int(std::max<int64_t>(std::min({want / batch, useful, room / batch, int64_t(FP4_SPLITS_MAX)}), 1));
     const int64_t groups = int64_t(a.flat ? chunks : batch) * a.splits;
     if (a.blocks > 65535 || groups > 65535) return KV_ERR_UNSUPPORTED;
-    const bool merged = a.splits > 1 && a.splits <= 64 && streams * batch <= FP4_COUNTERS && a.rows * a.splits <= FP4_MERGED_ROWS;
+    const bool merged = a.width == FP4_COLUMNS && a.splits > 1 && a.splits <= 64 && streams * batch <= FP4_COUNTERS && a.rows * a.splits <= FP4_MERGED_ROWS;
     a.counters = merged ? reinterpret_cast<uint8_t *>(c->workspace) : nullptr;
     a.part = c->workspace + FP4_COUNTERS / sizeof(float);
     const dim3 grid = dim3(uint32_t(v.H), uint32_t(a.blocks), uint32_t(groups));
 #define LAUNCH(HD, BF) hipLaunchKernelGGL((fp4_attention_kernel<HD, BF>), grid, dim3(256), 0, s, a)
-    if (c->cfg.head_dim == 128) {
+    if (a.width == FP4_TILE_COLUMNS) {
+        const int rc = launch_fp4_tiles(a, grid, c->cfg.head_dim, bf16, s);
+        if (rc) return rc;
+    } else if (c->cfg.head_dim == 128) {
         if (bf16) LAUNCH(128, true); else LAUNCH(128, false);
     } else {
         if (bf16) LAUNCH(64, true); else LAUNCH(64, false);
