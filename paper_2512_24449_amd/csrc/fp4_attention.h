@@ -25,9 +25,9 @@ typedef __bf16 bf168_t __attribute__((ext_vector_type(8)));
 typedef float float4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
 
-constexpr int FP4_STEP = 32;             // tokens of a step: half a page
+constexpr int FP4_STEP = 32;             // tokens of a step of the streaming kernel: half a page
 constexpr int FP4_COLUMNS = 16;          // of a product; of a block of the streaming kernel
-constexpr int FP4_TILE_COLUMNS = 128;    // of a block of the tile kernel
+constexpr int FP4_TILE_COLUMNS = 128;    // of a block of the tile kernel, whose steps are pages
 // Weights are relative to a maximum that follows the scores only when one is P_SLACK (in powers of two) above it: most steps
 // scale no sums then.  They are held as 2^P_LIFT times their size, so that the largest is between 2^12 and 2^15, and fp16
 // keeps its eleven bits down to 2^-26 of it.
@@ -161,8 +161,9 @@ __device__ inline void store_out(void *out, int type, int64_t at, const float (&
         *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(out) + at + 2 * i) = make_uint2(w[i], w[i + 1]);
 }
 
-// The tokens that a block of columns sees, in steps of 32: those that hold first tokens, then those from the window's
+// The tokens that a block of columns sees, in steps of UNIT (32 or 64): those that hold first tokens, then those from the window's
 // start to the last row.
+template <int UNIT>
 struct Fp4Steps {
     int first_row, last_row;   // new rows of the block
     int end;                   // tokens from here on are seen by none
@@ -174,11 +175,11 @@ struct Fp4Steps {
         last_row = min((column0 + columns - 1) / G, rows - 1);
         end = min(pos0 + last_row + 1, seq.held);
         begin = window ? max(max(pos0 + first_row, 0) - window + 1, 0) : 0;
-        window_step = begin / FP4_STEP;
-        sink_steps = min((min(window ? sinks : 0, max(end, 0)) + FP4_STEP - 1) / FP4_STEP, window_step);
-        n = end > 0 && first_row < rows ? sink_steps + max((end + FP4_STEP - 1) / FP4_STEP - window_step, 0) : 0;
+        window_step = begin / UNIT;
+        sink_steps = min((min(window ? sinks : 0, max(end, 0)) + UNIT - 1) / UNIT, window_step);
+        n = end > 0 && first_row < rows ? sink_steps + max((end + UNIT - 1) / UNIT - window_step, 0) : 0;
     }
-    __device__ inline int token(int step) const { return FP4_STEP * (step < sink_steps ? step : step - sink_steps + window_step); }
+    __device__ inline int token(int step) const { return UNIT * (step < sink_steps ? step : step - sink_steps + window_step); }
 };
 
 // sm_scale * log2(e) as the kernels use it.  A negative scale is one of -q: the largest scaled score is then that of the
@@ -205,17 +206,22 @@ struct Fp4Column {
         m = bar = -INFINITY;
         lift = P_LIFT;
     }
-    // Scores of the lane's eight tokens from t8 on: those that the column does not see count nothing.
-    __device__ inline void mask(float4_t (&s)[2], int t8, int end, int sinks) const {
+    // Scores of T / 2 times eight tokens, the first from t8 on, the next 32 further: those that the column does not see count
+    // nothing.
+    template <int T>
+    __device__ inline void mask(float4_t (&s)[T], int t8, int end, int sinks) const {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int t = t8 + i;
+        for (int i = 0; i < 4 * T; ++i) {
+            const int t = t8 + 32 * (i >> 3) + (i & 7);
             s[i >> 2][i & 3] = (t <= hi) & (t < end) & ((t >= lo) | (t < sinks)) ? s[i >> 2][i & 3] : -INFINITY;
         }
     }
-    // The tokens' weights as an operand.
-    __device__ inline uint4_t weigh(const float4_t (&s)[2], const Fp4Scale &scale) {
-        float top = max3(max3(s[0][0], s[0][1], s[0][2]), max3(s[0][3], s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]));
+    // The tokens' weights as operands.
+    template <int T>
+    __device__ inline void weigh(const float4_t (&s)[T], const Fp4Scale &scale, uint4_t (&p)[T / 2]) {
+        float top = fmaxf(s[0][0], s[0][1]);
+#pragma unroll
+        for (int i = 1; i < 2 * T; ++i) top = max3(top, s[i >> 1][2 * (i & 1)], s[i >> 1][2 * (i & 1) + 1]);
         if (__any(top > bar)) {
             top = column_max(top);
             if (top > bar) {
@@ -228,16 +234,13 @@ struct Fp4Column {
                 lift = P_LIFT - top * scale.scale;
             }
         }
-        half2_t p[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 2 * T; ++i) {
             const float x = __builtin_amdgcn_exp2f(fmaf(s[i >> 1][2 * (i & 1)], scale.scale, lift));
             const float y = __builtin_amdgcn_exp2f(fmaf(s[i >> 1][2 * (i & 1) + 1], scale.scale, lift));
             l += x + y;
-            p[i] = half2_t{_Float16(x), _Float16(y)};
+            p[i >> 2][i & 3] = __builtin_bit_cast(uint32_t, half2_t{_Float16(x), _Float16(y)});
         }
-        return uint4_t{__builtin_bit_cast(uint32_t, p[0]), __builtin_bit_cast(uint32_t, p[1]), __builtin_bit_cast(uint32_t, p[2]),
-                       __builtin_bit_cast(uint32_t, p[3])};
     }
     __device__ inline float scaled_max(const Fp4Scale &scale) const { return m == -INFINITY ? m : m * scale.scale; }
 };
@@ -264,6 +267,7 @@ struct Fp4Share {
     int b0, mine, before;    // the 64 sequences begin at b0; lane i: splits of sequence b0 + i, of those before it
     int len, rows, row0;     // and what the batch says of it
 
+    template <int UNIT>
     __device__ inline void find(const Fp4Attention &a, int chunk, int column0, int lane) {
         const kv_fp4_batch_t &t = a.v.batch;
         b0 = FP4_FLAT * chunk;
@@ -274,7 +278,7 @@ struct Fp4Share {
             len = t.lens[b0 + lane], rows = Fp4Sequence::raw_rows(a.v, b0 + lane), row0 = Fp4Sequence::raw_first(a.v, b0 + lane);
             const Fp4Sequence seq(a.v, b0 + lane, len, rows, row0);
             // (a row that sees nothing is written, too)
-            if (column0 < seq.n * a.v.G) steps = max(Fp4Steps(seq, column0, a.width, a.v.G, a.window, a.sinks).n, 1);
+            if (column0 < seq.n * a.v.G) steps = max(Fp4Steps<UNIT>(seq, column0, a.width, a.v.G, a.window, a.sinks).n, 1);
         }
         const float all = float(uint32_t(__builtin_amdgcn_readlane(wave_inclusive_scan(int(steps)), 63)));   // at most 64 * 2^25
         // quotients in fp32: U is too large rather than too small, the splits are then exact

@@ -45,7 +45,7 @@ struct Fp4Stage {
 // The page numbers of the next 64 steps of a wave, one to a lane: none of its transfers waits for the table.
 struct Fp4Pages {
     int page;                // (page numbers fit 31 bits) -1: missing
-    __device__ inline void load(const Fp4View &v, const Fp4Sequence &seq, const Fp4Steps &steps, int step, int end, int lane) {
+    __device__ inline void load(const Fp4View &v, const Fp4Sequence &seq, const Fp4Steps<FP4_STEP> &steps, int step, int end, int lane) {
         const int mine = step + 4 * lane;
         page = mine < end ? int(seq.page(v, steps.token(mine) / FP4_PAGE)) : -1;
     }
@@ -67,7 +67,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(F
     // (numbers of workgroups are the slowest axis: those without work come last and leave no compute unit out)
     const int chunk = int(blockIdx.z / uint32_t(a.splits)), group = int(blockIdx.z % uint32_t(a.splits));
     if (a.flat) {
-        share.find(a, chunk, column0, lane);
+        share.find<FP4_STEP>(a, chunk, column0, lane);
         share.of_group(group);
         if (share.splits == 0) return;
     } else {
@@ -76,7 +76,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(F
     const Fp4Sequence seq = a.flat ? share.sequence(v) : Fp4Sequence(v, share.b);
     const int columns = seq.n * v.G;
     if (column0 >= columns) return;
-    const Fp4Steps steps(seq, column0, FP4_COLUMNS, v.G, a.window, a.sinks);
+    const Fp4Steps<FP4_STEP> steps(seq, column0, FP4_COLUMNS, v.G, a.window, a.sinks);
     const int per_split = (steps.n + share.splits - 1) / share.splits;
     const int step_end = min((share.split + 1) * per_split, steps.n);
     int step = __builtin_amdgcn_readfirstlane(share.split * per_split + wave);
@@ -125,14 +125,15 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(F
 #pragma unroll
             for (int x = 0; x < VH; ++x) vs[x] = seen_scales(vs[x], t8, steps.begin, from.end, a.sinks);
         }
-        const uint4_t p = col.weigh(s, scale);
+        uint4_t p[1];
+        col.weigh(s, scale, p);
 #pragma unroll
         for (int x = 0; x < VH; ++x) {
             half2_t scales[4];
             scale_pairs(vs[x], scales);
             const uint32_t words[4] = {from.v[x].x, from.v[x].y, from.v[x].z, from.v[x].w};
 #pragma unroll
-            for (int c = 0; c < 4; ++c) col.o[4 * x + c] = product16<false>(column_operand(words[c], scales), p, col.o[4 * x + c]);
+            for (int c = 0; c < 4; ++c) col.o[4 * x + c] = product16<false>(column_operand(words[c], scales), p[0], col.o[4 * x + c]);
         }
     };
     for (; step < step_end; step += 4 * 64) {
@@ -276,7 +277,8 @@ __global__ __launch_bounds__(256) void fp4_join_kernel(Fp4Attention a) {
     Fp4Share share;
     share.splits = a.splits, share.first = 0;
     if (a.flat) {
-        share.find(a, b / FP4_FLAT, column / a.width * a.width, lane);
+        if (a.width == FP4_TILE_COLUMNS) share.find<FP4_PAGE>(a, b / FP4_FLAT, column / a.width * a.width, lane);
+        else share.find<FP4_STEP>(a, b / FP4_FLAT, column / a.width * a.width, lane);
         share.of_sequence(b);
     }
     const int splits = share.splits;
@@ -362,8 +364,9 @@ int launch_fp4_attention(const kv_fp4_cache *c, const Fp4View &v, const void *q,
     a.blocks = int((columns + a.width - 1) / a.width);
     a.rows = int(std::min<int64_t>(columns, a.width));
     // Steps that a block of columns can have.
-    int64_t most = int64_t(v.batch.table_pages) * (FP4_PAGE / FP4_STEP);
-    if (window) most = std::min(most, (int64_t(window) + a.width + sinks) / FP4_STEP + 3);
+    const int unit = a.width == FP4_TILE_COLUMNS ? FP4_PAGE : FP4_STEP;
+    int64_t most = int64_t(v.batch.table_pages) * (FP4_PAGE / unit);
+    if (window) most = std::min(most, (int64_t(window) + a.width + sinks) / unit + 3);
     const int batch = v.batch.batch;
     const int64_t streams = int64_t(a.blocks) * v.H, room = FP4_PART_ROWS / a.rows / streams;   // workgroups that the workspace takes
     a.least_steps = streams * batch * (most / FP4_LEAST_STEPS) <= FP4_FEW_GROUPS ? FP4_LEAST_STEPS : FP4_MORE_STEPS;

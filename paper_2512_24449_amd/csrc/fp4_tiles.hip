@@ -1,5 +1,5 @@
 // Attention over the 4-bit paged cache for many new rows (drafts, chunks of a prompt, prompts): a workgroup takes 128 columns, a
-// wave 32 of them.  Bound by the vector instructions of the softmax and by the matrix cores; what a tile of 32 tokens costs once
+// wave 32 of them.  Bound by the vector instructions of the softmax and by the matrix cores; what a tile (a page, 64 tokens) costs once
 // -- its transfer and its conversion to fp16 -- is shared by the four waves through LDS, where it lies as the operands that
 // the products take: every wave reads 16 bytes a lane, a kilobyte in a row.  Two tiles in turn, one barrier each: while one is
 // multiplied, the next is converted and the one after that is on its way.
@@ -7,56 +7,57 @@
 
 namespace packkv {
 
-// A wave's quarter of a tile on its way: words of K and V that it will convert.
+// A wave's quarter of a tile on its way: the K of 16 tokens, the V of 32 tokens and half the channels.
 template <int HD>
 struct Fp4Quarter {
     using P = Fp4Block<HD>;
-    static constexpr int KW = HD / 32, OT = HD / 16, KN = KW / 2, VN = OT / 4;   // operands of K and of V that a wave makes
-    uint32_t k[KN], v[VN];
+    static constexpr int KW = HD / 32, OT = HD / 16, VN = OT / 2;   // operands of 16 tokens' K, of 32 tokens' V; of V that a wave makes
+    uint32_t k[KW], v[VN];
     uint32_t ks;
     uint2 vs;
     int t0, end;             // as of Fp4Stage
 
-    __device__ inline void load(const uint8_t *block, int at, int wave, int c16, int g) {
-        // K: operands KN wave .. of 2 KW, KW to each 16 tokens; V: operands VN wave .. of OT, four to each 64 channels
-        const int token = 8 * (c16 >> 2) + (c16 & 3) + 4 * (wave >> 1);
-        const uint8_t *kp = block + P::K + (at + token) * (HD / 2) + g * (HD / 8) + 4 * KN * (wave & 1);
-        ks = block[P::KS + (at + token) * (HD / FP4_GROUP) + g * (HD / 4) / FP4_GROUP];
-        const int x = VN * wave / 4, c = VN * wave % 4;
-        const uint8_t *vp = block + P::V + at * (HD / 2) + (g * HD + 64 * x + 4 * c16 + c) * 4;
+    __device__ inline void load(const uint8_t *block, int wave, int c16, int g) {
+        // operand o of K or V is row o % 2 of half o / 2 of the page: tokens 8g + 4 (wave % 2) + .. of the half, its channels
+        const int half = 32 * (wave >> 1), token = half + 8 * (c16 >> 2) + (c16 & 3) + 4 * (wave & 1);
+        const uint8_t *kp = block + P::K + token * (HD / 2) + g * (HD / 8);
+        ks = block[P::KS + token * (HD / FP4_GROUP) + g * (HD / 4) / FP4_GROUP];
+        const int x = HD == 128 ? wave & 1 : 0, c = HD == 128 ? 0 : 2 * (wave & 1);   // V: 64 channels, four (two) operands of them
+        const uint8_t *vp = block + P::V + half * (HD / 2) + (g * HD + 64 * x + 4 * c16 + c) * 4;
         if constexpr (HD == 128) {
+            const uint4 a = *reinterpret_cast<const uint4 *>(kp), b = *reinterpret_cast<const uint4 *>(vp);
+            k[0] = a.x, k[1] = a.y, k[2] = a.z, k[3] = a.w, v[0] = b.x, v[1] = b.y, v[2] = b.z, v[3] = b.w;
+        } else {
             const uint2 a = *reinterpret_cast<const uint2 *>(kp), b = *reinterpret_cast<const uint2 *>(vp);
             k[0] = a.x, k[1] = a.y, v[0] = b.x, v[1] = b.y;
-        } else {
-            k[0] = *reinterpret_cast<const uint32_t *>(kp), v[0] = *reinterpret_cast<const uint32_t *>(vp);
         }
-        vs = *reinterpret_cast<const uint2 *>(block + P::VS + (2 * x + (c16 >> 3)) * FP4_PAGE + at + 8 * g);
+        vs = *reinterpret_cast<const uint2 *>(block + P::VS + (2 * x + (c16 >> 3)) * FP4_PAGE + half + 8 * g);
     }
-    // tile: 2 KW + OT operands of 64 x 16 bytes, K's first
+    // tile: 4 KW operands of K (64 x 16 bytes each), 2 OT of V
     template <bool BF16>
     __device__ inline void store(uint4_t (*tile)[64], int wave, int lane) const {
         const float scale = __uint_as_float(ks << 23);
 #pragma unroll
-        for (int i = 0; i < KN; ++i) tile[KN * wave + i][lane] = row_operand<BF16>(k[i], scale);
+        for (int i = 0; i < KW; ++i) tile[KW * wave + i][lane] = row_operand<BF16>(k[i], scale);
         half2_t scales[4];
         scale_pairs(vs, scales);
 #pragma unroll
-        for (int i = 0; i < VN; ++i) tile[2 * KW + VN * wave + i][lane] = column_operand(v[i], scales);
+        for (int i = 0; i < VN; ++i) tile[4 * KW + VN * wave + i][lane] = column_operand(v[i], scales);
     }
 };
 
 // Page numbers of the steps to come, 64 to a register, the register after it loaded 64 steps ahead.
 struct Fp4PagesAhead {
     int now, next, base;
-    __device__ inline int load(const Fp4View &v, const Fp4Sequence &seq, const Fp4Steps &steps, int from, int end, int lane) {
+    __device__ inline int load(const Fp4View &v, const Fp4Sequence &seq, const Fp4Steps<FP4_PAGE> &steps, int from, int end, int lane) {
         return from + lane < end ? int(seq.page(v, steps.token(from + lane) / FP4_PAGE)) : -1;
     }
-    __device__ inline void start(const Fp4View &v, const Fp4Sequence &seq, const Fp4Steps &steps, int from, int end, int lane) {
+    __device__ inline void start(const Fp4View &v, const Fp4Sequence &seq, const Fp4Steps<FP4_PAGE> &steps, int from, int end, int lane) {
         base = from;
         now = load(v, seq, steps, from, end, lane);
         next = load(v, seq, steps, from + 64, end, lane);
     }
-    __device__ inline int at(const Fp4View &v, const Fp4Sequence &seq, const Fp4Steps &steps, int step, int end, int lane) {   // steps in order
+    __device__ inline int at(const Fp4View &v, const Fp4Sequence &seq, const Fp4Steps<FP4_PAGE> &steps, int step, int end, int lane) {   // steps in order
         if (step - base >= 64) {
             base += 64;
             now = next;
@@ -70,7 +71,7 @@ template <int HD, bool BF16>
 __global__ __launch_bounds__(256, HD == 128 ? 2 : 3) void fp4_tile_kernel(Fp4Attention a) {
     using P = Fp4Block<HD>;
     constexpr int KW = HD / 32, VH = HD / 64, OT = HD / 16, NB = FP4_TILE_COLUMNS / 64;
-    __shared__ uint4_t tiles[2][2 * KW + OT][64];
+    __shared__ uint4_t tiles[2][4 * KW + 2 * OT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c16 = lane & 15, g = lane >> 4;
     const Fp4View &v = a.v;
     const int h = blockIdx.x, block = int(blockIdx.y), column0 = block * FP4_TILE_COLUMNS;
@@ -78,7 +79,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : 3) void fp4_tile_kernel(Fp4Att
     Fp4Share share;
     const int chunk = int(blockIdx.z / uint32_t(a.splits)), group = int(blockIdx.z % uint32_t(a.splits));
     if (a.flat) {
-        share.find(a, chunk, column0, lane);
+        share.find<FP4_PAGE>(a, chunk, column0, lane);
         share.of_group(group);
         if (share.splits == 0) return;
     } else {
@@ -87,7 +88,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : 3) void fp4_tile_kernel(Fp4Att
     const Fp4Sequence seq = a.flat ? share.sequence(v) : Fp4Sequence(v, share.b);
     const int columns = seq.n * v.G;
     if (column0 >= columns) return;
-    const Fp4Steps steps(seq, column0, FP4_TILE_COLUMNS, v.G, a.window, a.sinks);
+    const Fp4Steps<FP4_PAGE> steps(seq, column0, FP4_TILE_COLUMNS, v.G, a.window, a.sinks);
     const int per_split = (steps.n + share.splits - 1) / share.splits;
     const int step0 = share.split * per_split, step_end = min(step0 + per_split, steps.n);
 
@@ -118,11 +119,11 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : 3) void fp4_tile_kernel(Fp4Att
         const int page = pages.at(v, seq, steps, step, step_end, lane);
         in.t0 = steps.token(step);
         in.end = page < 0 ? 0 : steps.end;
-        in.load(v.pages + (int64_t(max(page, 0)) * v.H + h) * size_t(P::BYTES), in.t0 % FP4_PAGE, wave, c16, g);
+        in.load(v.pages + (int64_t(max(page, 0)) * v.H + h) * size_t(P::BYTES), wave, c16, g);
     };
     auto convert = [&](int to) {
-        if (in.t0 + FP4_STEP > in.end || in.t0 < steps.begin)
-            in.vs = seen_scales(in.vs, in.t0 + 8 * g, steps.begin, in.end, a.sinks);
+        if (in.t0 + FP4_PAGE > in.end || in.t0 < steps.begin)
+            in.vs = seen_scales(in.vs, in.t0 + 32 * (wave >> 1) + 8 * g, steps.begin, in.end, a.sinks);
         in.template store<BF16>(tiles[to], wave, lane);
     };
     int t0 = 0, end = 0;
@@ -139,31 +140,43 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : 3) void fp4_tile_kernel(Fp4Att
         convert(now ^ 1);    // (behind the last tile that one again, which nobody reads)
         const int next_t0 = in.t0, next_end = in.end;
         fetch(min(step + 2, step_end - 1));
-        if (wave_columns > 0 && t0 <= last_hi && (t0 + FP4_STEP > first_lo || t0 < a.sinks)) {
-            float4_t s[NB][2];
+        if (wave_columns > 0 && t0 <= last_hi && (t0 + FP4_PAGE > first_lo || t0 < a.sinks)) {
+            // Operands are read ahead of the products: K's of 32 tokens, the others as those are used, V's of 32 tokens before
+            // the softmax.
+            const uint4_t(*tile)[64] = tiles[now];
+            uint4_t f[2 * KW];
+            float4_t s[NB][4];
 #pragma unroll
-            for (int n = 0; n < NB; ++n) s[n][0] = s[n][1] = float4_t{0, 0, 0, 0};
+            for (int i = 0; i < 2 * KW; ++i) f[i] = tile[i][lane];
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < 4; ++t) {
+#pragma unroll
+                for (int n = 0; n < NB; ++n) s[n][t] = float4_t{0, 0, 0, 0};
 #pragma unroll
                 for (int i = 0; i < KW; ++i) {
-                    const uint4_t k = tiles[now][t * KW + i][lane];
+                    const uint4_t k = f[t % 2 * KW + i];
 #pragma unroll
                     for (int n = 0; n < NB; ++n) s[n][t] = product16<BF16>(k, q[n][i], s[n][t]);
+                    f[t % 2 * KW + i] = tile[(t + 2) * KW + i][lane];   // (behind K: V's first)
                 }
-            if (t0 + FP4_STEP > min(end, first_hi + 1) || t0 < last_lo) {
+            }
+            static_assert(OT == 2 * KW, "as many operands of V for 32 tokens as of K");
+            if (t0 + FP4_PAGE > min(end, first_hi + 1) || t0 < last_lo) {
 #pragma unroll
                 for (int n = 0; n < NB; ++n) col[n].mask(s[n], t0 + 8 * g, end, a.sinks);
             }
-            uint4_t p[NB];
+            uint4_t p[NB][2];
 #pragma unroll
-            for (int n = 0; n < NB; ++n) p[n] = col[n].weigh(s[n], scale);
+            for (int n = 0; n < NB; ++n) col[n].weigh(s[n], scale, p[n]);
 #pragma unroll
-            for (int i = 0; i < OT; ++i) {
-                const uint4_t w = tiles[now][2 * KW + i][lane];
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int n = 0; n < NB; ++n) col[n].o[i] = product16<false>(w, p[n], col[n].o[i]);
-            }
+                for (int i = 0; i < OT; ++i) {
+                    const uint4_t w = f[i];
+                    if (u == 0) f[i] = tile[4 * KW + OT + i][lane];
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) col[n].o[i] = product16<false>(w, p[n][u], col[n].o[i]);
+                }
         }
         t0 = next_t0, end = next_end;
         __syncthreads();
