@@ -148,18 +148,22 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : 3) void fp4_tile_kernel(Fp4Att
             float4_t s[NB][4];
 #pragma unroll
             for (int i = 0; i < 2 * KW; ++i) f[i] = tile[i][lane];
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
+            for (int u = 0; u < 2; ++u) {
 #pragma unroll
-                for (int n = 0; n < NB; ++n) s[n][t] = float4_t{0, 0, 0, 0};
+                for (int n = 0; n < NB; ++n) s[n][2 * u] = s[n][2 * u + 1] = float4_t{0, 0, 0, 0};
 #pragma unroll
-                for (int i = 0; i < KW; ++i) {
-                    const uint4_t k = f[t % 2 * KW + i];
+                for (int i = 0; i < KW; ++i)
 #pragma unroll
-                    for (int n = 0; n < NB; ++n) s[n][t] = product16<BF16>(k, q[n][i], s[n][t]);
-                    f[t % 2 * KW + i] = tile[(t + 2) * KW + i][lane];   // (behind K: V's first)
-                }
+                    for (int t = 0; t < 2; ++t) {
+                        const uint4_t k = f[t * KW + i];
+#pragma unroll
+                        for (int n = 0; n < NB; ++n) s[n][2 * u + t] = product16<BF16>(k, q[n][i], s[n][2 * u + t]);
+                        f[t * KW + i] = tile[(2 * u + 2 + t) * KW + i][lane];   // (behind K: V's first)
+                    }
             }
+            __builtin_amdgcn_s_setprio(0);
             static_assert(OT == 2 * KW, "as many operands of V for 32 tokens as of K");
             if (t0 + FP4_PAGE > min(end, first_hi + 1) || t0 < last_lo) {
 #pragma unroll
@@ -168,6 +172,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : 3) void fp4_tile_kernel(Fp4Att
             uint4_t p[NB][2];
 #pragma unroll
             for (int n = 0; n < NB; ++n) col[n].weigh(s[n], scale, p[n]);
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -177,6 +182,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : 3) void fp4_tile_kernel(Fp4Att
 #pragma unroll
                     for (int n = 0; n < NB; ++n) col[n].o[i] = product16<false>(w, p[n][u], col[n].o[i]);
                 }
+            __builtin_amdgcn_s_setprio(0);
         }
         t0 = next_t0, end = next_end;
         __syncthreads();
