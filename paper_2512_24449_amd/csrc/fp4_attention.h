@@ -35,7 +35,7 @@ constexpr float P_LIFT = 12.0f, P_SLACK = 3.0f;
 // The workspace: a counter byte for each of so many (stream, sequence) pairs whose splits are joined by the last workgroup
 // of them, and partial results, at most so many rows (of a column in a split) of HD + 4 floats.
 constexpr int FP4_COUNTERS = 4096;
-constexpr int64_t FP4_PART_ROWS = 32768;
+constexpr int64_t FP4_PART_ROWS = 65536;
 constexpr int FP4_SPLITS_MAX = 256;
 // Sequences that share workgroups by their lengths.
 constexpr int FP4_FLAT = 64;
@@ -43,6 +43,8 @@ constexpr int FP4_FLAT = 64;
 // head x 1000 tokens 7.8 / 8.5 us, 32 heads x 4100 14.8 / 13.2, a window of 4096 of 8 kv-heads 10.0 / 9.6.
 constexpr int FP4_LEAST_STEPS = 8, FP4_MORE_STEPS = 12;
 constexpr int64_t FP4_FEW_GROUPS = 128;
+// Steps of a split that more workgroups than fit at once may have: then its start costs little.
+constexpr int FP4_LONG_STEPS = 64;
 
 struct Fp4Attention {
     Fp4View v;
@@ -57,7 +59,9 @@ struct Fp4Attention {
     uint8_t *counters;       // not null: the last workgroup of a sequence joins its splits
     int width, blocks;       // columns of a block, blocks; a stream is a block of a kv-head
     int rows;                // columns of a block with partial results: all, or what max_new has
-    int least_steps;         // of a split (flat)
+    int least_steps;         // of a split
+    int few;                 // splits of all sequences that share, where those have FP4_LONG_STEPS or fewer
+    int most_splits;         // of a sequence
     bool flat;               // the workgroups of 64 sequences of a stream go to them by their lengths; else each has as many
     int splits;              // workgroups of those; or of a stream and sequence
 
@@ -260,20 +264,38 @@ __device__ inline uint2 seen_scales(uint2 bytes, int t8, int begin, int end, int
 // Which sequence a workgroup works for, and which of how many splits of its steps.  Flat: the workgroups of 64 sequences of
 // a stream are shared out so that none has more steps than some U >= all steps / (workgroups - sequences): the sum of
 // ceil(steps / U) is then at most the workgroups, and a long sequence among short ones has more of them.  Every wave finds
-// the shares by itself, a sequence to a lane.
+// the shares by itself, a sequence to a lane.  Else a sequence has the workgroups to itself, and again takes as many as U says.
+template <int UNIT>
 struct Fp4Share {
     int b, split, splits;    // splits 0: no work
     int first;               // flat: the sequence's first workgroup among those of the 64
-    int b0, mine, before;    // the 64 sequences begin at b0; lane i: splits of sequence b0 + i, of those before it
-    int len, rows, row0;     // and what the batch says of it
 
-    template <int UNIT>
-    __device__ inline void find(const Fp4Attention &a, int chunk, int column0, int lane) {
+    // U and ceil(steps / U), with quotients in fp32: U is too large rather than too small, the splits are then exact
+    static __device__ inline uint32_t steps_of_split(const Fp4Attention &a, float all, int room) {
+        const auto over = [&](int n) { return uint32_t(all * __builtin_amdgcn_rcpf(float(n)) * (1.0f + 0x1p-20f)) + 1; };
+        return max(max(over(room), min(over(a.few), uint32_t(FP4_LONG_STEPS))), uint32_t(a.least_steps));
+    }
+    static __device__ inline int splits_of(const Fp4Attention &a, uint32_t steps, uint32_t of_split) {
+        // (the quotient is below 2^11, or the splits below are the most: off by one at most)
+        uint32_t q = uint32_t(float(steps) * __builtin_amdgcn_rcpf(float(of_split)));
+        q = q * of_split < steps ? q + 1 : q;
+        return min(int(q * of_split < steps ? q + 1 : q), a.most_splits);
+    }
+
+    // For workgroup `group` of sequence (or 64 sequences) `chunk`, or, group -1, for sequence `sequence`.
+    __device__ inline Fp4Sequence find(const Fp4Attention &a, int chunk, int group, int sequence, int column0, int lane) {
         const kv_fp4_batch_t &t = a.v.batch;
-        b0 = FP4_FLAT * chunk;
-        const int here = min(t.batch - b0, FP4_FLAT);
+        if (!a.flat) {
+            b = chunk, split = group, first = 0;
+            const Fp4Sequence seq(a.v, b);
+            const uint32_t steps = column0 < seq.n * a.v.G ? max(Fp4Steps<UNIT>(seq, column0, a.width, a.v.G, a.window, a.sinks).n, 1) : 0;
+            splits = splits_of(a, steps, steps_of_split(a, float(steps), a.splits));
+            if (group >= splits) splits = 0;
+            return seq;
+        }
+        const int b0 = FP4_FLAT * chunk, here = min(t.batch - b0, FP4_FLAT);
         uint32_t steps = 0;
-        len = rows = row0 = 0;
+        int len = 0, rows = 0, row0 = 0;
         if (lane < here) {
             len = t.lens[b0 + lane], rows = Fp4Sequence::raw_rows(a.v, b0 + lane), row0 = Fp4Sequence::raw_first(a.v, b0 + lane);
             const Fp4Sequence seq(a.v, b0 + lane, len, rows, row0);
@@ -281,28 +303,19 @@ struct Fp4Share {
             if (column0 < seq.n * a.v.G) steps = max(Fp4Steps<UNIT>(seq, column0, a.width, a.v.G, a.window, a.sinks).n, 1);
         }
         const float all = float(uint32_t(__builtin_amdgcn_readlane(wave_inclusive_scan(int(steps)), 63)));   // at most 64 * 2^25
-        // quotients in fp32: U is too large rather than too small, the splits are then exact
-        const uint32_t most = max(uint32_t(all * __builtin_amdgcn_rcpf(float(a.splits - here)) * (1.0f + 0x1p-20f)) + 1, uint32_t(a.least_steps));
-        uint32_t q = uint32_t(float(steps) * __builtin_amdgcn_rcpf(float(most)));      // at most 2^8: off by one at most
-        q = q * most < steps ? q + 1 : q;
-        mine = int(q * most < steps ? q + 1 : q);
-        before = wave_inclusive_scan(mine) - mine;
-    }
-    __device__ inline void of_sequence(int sequence) {
-        b = sequence;
-        splits = __builtin_amdgcn_readlane(mine, b - b0);
-        first = __builtin_amdgcn_readlane(before, b - b0);
-    }
-    __device__ inline void of_group(int group) {
-        const uint64_t has = __ballot(before <= group && group < before + mine);
-        splits = 0;
-        if (!has) return;
-        of_sequence(b0 + __builtin_ctzll(has));
+        const int mine = splits_of(a, steps, steps_of_split(a, all, a.splits - here)), before = wave_inclusive_scan(mine) - mine;
+        int at = sequence - b0;
+        if (group >= 0) {
+            const uint64_t has = __ballot(before <= group && group < before + mine);
+            at = has ? __builtin_ctzll(has) : 0;
+        }
+        b = b0 + at;
+        splits = __builtin_amdgcn_readlane(mine, at);
+        first = __builtin_amdgcn_readlane(before, at);
         split = group - first;
-    }
-    __device__ inline Fp4Sequence sequence(const Fp4View &v) const {
-        return Fp4Sequence(v, b, __builtin_amdgcn_readlane(len, b - b0), __builtin_amdgcn_readlane(rows, b - b0),
-                           __builtin_amdgcn_readlane(row0, b - b0));
+        if (group >= 0 && uint32_t(split) >= uint32_t(splits)) splits = 0;
+        return Fp4Sequence(a.v, b, __builtin_amdgcn_readlane(len, at), __builtin_amdgcn_readlane(rows, at),
+                           __builtin_amdgcn_readlane(row0, at));
     }
 };
 

@@ -63,19 +63,11 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(F
     __shared__ uint32_t lds_last;
     const int h = blockIdx.x, block = int(blockIdx.y), column0 = block * FP4_COLUMNS;
     const uint32_t stream = uint32_t(block) * v.H + h;
-    Fp4Share share;
     // (numbers of workgroups are the slowest axis: those without work come last and leave no compute unit out)
-    const int chunk = int(blockIdx.z / uint32_t(a.splits)), group = int(blockIdx.z % uint32_t(a.splits));
-    if (a.flat) {
-        share.find<FP4_STEP>(a, chunk, column0, lane);
-        share.of_group(group);
-        if (share.splits == 0) return;
-    } else {
-        share.b = chunk, share.split = group, share.splits = a.splits, share.first = 0;
-    }
-    const Fp4Sequence seq = a.flat ? share.sequence(v) : Fp4Sequence(v, share.b);
+    Fp4Share<FP4_STEP> share;
+    const Fp4Sequence seq = share.find(a, int(blockIdx.z / uint32_t(a.splits)), int(blockIdx.z % uint32_t(a.splits)), 0, column0, lane);
+    if (share.splits == 0) return;
     const int columns = seq.n * v.G;
-    if (column0 >= columns) return;
     const Fp4Steps<FP4_STEP> steps(seq, column0, FP4_COLUMNS, v.G, a.window, a.sinks);
     const int per_split = (steps.n + share.splits - 1) / share.splits;
     const int step_end = min((share.split + 1) * per_split, steps.n);
@@ -274,18 +266,17 @@ __global__ __launch_bounds__(256) void fp4_join_kernel(Fp4Attention a) {
     const Fp4View &v = a.v;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int column = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
-    Fp4Share share;
-    share.splits = a.splits, share.first = 0;
-    if (a.flat) {
-        if (a.width == FP4_TILE_COLUMNS) share.find<FP4_PAGE>(a, b / FP4_FLAT, column / a.width * a.width, lane);
-        else share.find<FP4_STEP>(a, b / FP4_FLAT, column / a.width * a.width, lane);
-        share.of_sequence(b);
-    }
-    const int splits = share.splits;
-    const Fp4Sequence seq = a.flat ? share.sequence(v) : Fp4Sequence(v, b);
+    const int chunk = a.flat ? b / FP4_FLAT : b, column0 = column / a.width * a.width;
+    int splits, first;
+    const auto find = [&](auto share) {
+        const Fp4Sequence seq = share.find(a, chunk, -1, b, column0, lane);
+        splits = share.splits, first = share.first;
+        return seq;
+    };
+    const Fp4Sequence seq = a.width == FP4_TILE_COLUMNS ? find(Fp4Share<FP4_PAGE>()) : find(Fp4Share<FP4_STEP>());
     const int64_t out_row = seq.first + column / v.G;
     if (splits <= 1 || column >= seq.n * v.G || out_row < 0 || out_row >= v.n_rows) return;
-    const float *rows = a.part + a.part_row(column / a.width * v.H + h, b, share.first, column % a.width) * (HD + 4);
+    const float *rows = a.part + a.part_row(column / a.width * v.H + h, b, first, column - column0) * (HD + 4);
     const int64_t pitch = int64_t(a.rows) * (HD + 4);
     const int s = threadIdx.x;
     static_assert(FP4_SPLITS_MAX <= 256, "a thread to a split");
@@ -340,10 +331,13 @@ int launch_fp4_clear(const kv_fp4_cache *c, hipStream_t s) {
 
 // Columns of a kv-head up to which the streaming kernel takes them (in blocks of 16, each a pass over the cache).
 constexpr int64_t FP4_FEW_COLUMNS = 32;
-// Workgroups that a call is split into at most: not quite two to each of the 256 compute units (a third one on some of them
-// would hold up the call).  Four sequences of up to 32788 tokens, 8 kv-heads: 480 workgroups 26.9 us, 512 28.3, 256 27.1, 768 29.
-constexpr int64_t FP4_GROUPS = 480;
-// The last workgroup of a sequence joins its splits itself up to so many rows of partial results; beyond, a kernel with a
+// Workgroups that a call is split into: not quite two to each of the 256 compute units (a third one on some of them would hold
+// up the call), or more than fit at once (those end at different times, so that no compute unit is left without) where
+// that leaves FP4_LONG_STEPS to each.  Four sequences of up to 32788 tokens, 8 kv-heads: 480 workgroups 26.9 us, 512 28.3, 256
+// 27.1, 768 29.
+constexpr int64_t FP4_GROUPS = 480, FP4_MORE_GROUPS = 1536;
+// The last workgroup of a sequence joins its splits itself where twice its fair share of them makes so many rows of partial
+// results at most (it has no more then); beyond, a kernel with a
 // workgroup to each row of the output does.  Passes joined so / by the kernel: one head x 1000 tokens 7.8 / 8.6 us, a window
 // of 4096 of 8 kv-heads in 11 splits 9.6 / 10.6, four sequences of up to 32788 28.3 / 29, 32 heads x 4100 in 11 splits 13.2 /
 // 13.0; where no sequence turns out to be split (8 sequences x 52 heads) the kernel would be launched for nothing.
@@ -372,16 +366,24 @@ int launch_fp4_attention(const kv_fp4_cache *c, const Fp4View &v, const void *q,
     a.least_steps = streams * batch * (most / FP4_LEAST_STEPS) <= FP4_FEW_GROUPS ? FP4_LEAST_STEPS : FP4_MORE_STEPS;
     const int64_t useful = (most + a.least_steps - 1) / a.least_steps;       // splits of a sequence
     const int chunk = std::min(batch, FP4_FLAT), chunks = (batch + FP4_FLAT - 1) / FP4_FLAT;
-    int64_t want = FP4_GROUPS / streams;
+    const int64_t want = FP4_GROUPS / streams, more = FP4_MORE_GROUPS / streams;
     a.flat = batch > 1 && useful > 1 && room >= 2 * chunk * chunks;
-    if (a.flat)
-        a.splits = int(std::min({std::max<int64_t>(want / chunks, 2 * chunk), chunk * (1 + useful), room / chunks, int64_t(FP4_SPLITS_MAX)}));
-    else
-        a.splits = int(std::max<int64_t>(std::min({want / batch, useful, room / batch, int64_t(FP4_SPLITS_MAX)}), 1));
+    if (a.flat) {
+        a.splits = int(std::min({std::max<int64_t>(more / chunks, 2 * chunk), chunk * (1 + useful), room / chunks}));
+        a.few = int(std::max<int64_t>(want / chunks - chunk, 1));
+    } else {
+        a.splits = int(std::max<int64_t>(std::min({more / batch, useful, room / batch, int64_t(FP4_SPLITS_MAX)}), 1));
+        a.few = int(std::max<int64_t>(want / batch, 1));
+    }
+    a.most_splits = FP4_SPLITS_MAX;
     const int64_t groups = int64_t(a.flat ? chunks : batch) * a.splits;
     if (a.blocks > 65535 || groups > 65535) return KV_ERR_UNSUPPORTED;
-    const bool merged = a.width == FP4_COLUMNS && a.splits > 1 && a.splits <= 64 && streams * batch <= FP4_COUNTERS && a.rows * a.splits <= FP4_MERGED_ROWS;
-    a.counters = merged ? reinterpret_cast<uint8_t *>(c->workspace) : nullptr;
+    a.counters = nullptr;
+    const int64_t alone = std::min<int64_t>(64, FP4_MERGED_ROWS / a.rows), fair = std::min(useful, std::max<int64_t>(want / batch, 1));
+    if (a.width == FP4_COLUMNS && a.splits > 1 && streams * batch <= FP4_COUNTERS && 2 * fair <= alone) {
+        a.counters = reinterpret_cast<uint8_t *>(c->workspace);
+        a.most_splits = int(alone);
+    }
     a.part = c->workspace + FP4_COUNTERS / sizeof(float);
     const dim3 grid = dim3(uint32_t(v.H), uint32_t(a.blocks), uint32_t(groups));
 #define LAUNCH(HD, BF) hipLaunchKernelGGL((fp4_attention_kernel<HD, BF>), grid, dim3(256), 0, s, a)

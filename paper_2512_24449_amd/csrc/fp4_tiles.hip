@@ -76,18 +76,10 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : 3) void fp4_tile_kernel(Fp4Att
     const Fp4View &v = a.v;
     const int h = blockIdx.x, block = int(blockIdx.y), column0 = block * FP4_TILE_COLUMNS;
     const uint32_t stream = uint32_t(block) * v.H + h;
-    Fp4Share share;
-    const int chunk = int(blockIdx.z / uint32_t(a.splits)), group = int(blockIdx.z % uint32_t(a.splits));
-    if (a.flat) {
-        share.find<FP4_PAGE>(a, chunk, column0, lane);
-        share.of_group(group);
-        if (share.splits == 0) return;
-    } else {
-        share.b = chunk, share.split = group, share.splits = a.splits, share.first = 0;
-    }
-    const Fp4Sequence seq = a.flat ? share.sequence(v) : Fp4Sequence(v, share.b);
+    Fp4Share<FP4_PAGE> share;
+    const Fp4Sequence seq = share.find(a, int(blockIdx.z / uint32_t(a.splits)), int(blockIdx.z % uint32_t(a.splits)), 0, column0, lane);
+    if (share.splits == 0) return;
     const int columns = seq.n * v.G;
-    if (column0 >= columns) return;
     const Fp4Steps<FP4_PAGE> steps(seq, column0, FP4_TILE_COLUMNS, v.G, a.window, a.sinks);
     const int per_split = (steps.n + share.splits - 1) / share.splits;
     const int step0 = share.split * per_split, step_end = min(step0 + per_split, steps.n);
