@@ -43,6 +43,7 @@ constexpr int FP4_FLAT = 64;
 // head x 1000 tokens 7.8 / 8.5 us, 32 heads x 4100 14.8 / 13.2, a window of 4096 of 8 kv-heads 10.0 / 9.6.
 constexpr int FP4_LEAST_STEPS = 8, FP4_MORE_STEPS = 12;
 constexpr int64_t FP4_FEW_GROUPS = 128;
+constexpr int FP4_LEAST_PAGES = 4;       // the same, of the tile kernel
 // Steps of a split that more workgroups than fit at once may have: then its start costs little.
 constexpr int FP4_LONG_STEPS = 64;
 

@@ -329,8 +329,11 @@ int launch_fp4_clear(const kv_fp4_cache *c, hipStream_t s) {
     return KV_OK;
 }
 
-// Columns of a kv-head up to which the streaming kernel takes them (in blocks of 16, each a pass over the cache).
-constexpr int64_t FP4_FEW_COLUMNS = 32;
+// Which kernel: a block of 128 columns takes the tile kernel as long as five to six passes over the cache for 16 columns take
+// the streaming kernel, if there are workgroups for all compute units -- blocks enough, or splits of a long context.  Tile /
+// streaming kernel, heads of 128 (64): 16 sequences of 2000 tokens, 32 kv-heads, 64 columns each 104 / 79 us (85 / 49), 96 columns
+// 81 / 103 (59 / 64), 128 columns 86 / 133 (61 / 83); 64 of 4000 tokens, 8 kv-heads, 96 columns 141 / 188 (102 / 118); one of
+// 30000, 8 kv-heads, 256 columns 60 / 70 (43 / 46); one of 2000, 8 kv-heads, 512 columns 31 / 16 (27 / 12).
 // Workgroups that a call is split into: not quite two to each of the 256 compute units (a third one on some of them would hold
 // up the call), or more than fit at once (those end at different times, so that no compute unit is left without) where
 // that leaves FP4_LONG_STEPS to each.  Four sequences of up to 32788 tokens, 8 kv-heads: 480 workgroups 26.9 us, 512 28.3, 256
@@ -354,16 +357,19 @@ int launch_fp4_attention(const kv_fp4_cache *c, const Fp4View &v, const void *q,
     a.scale = sm_scale * 1.4426950408889634f;
     a.window = window, a.sinks = sinks;
     a.out = out, a.out_type = out_type, a.lse = lse;
-    a.width = columns > FP4_FEW_COLUMNS ? FP4_TILE_COLUMNS : FP4_COLUMNS;
+    const int batch = v.batch.batch;
+    const int64_t tiles = (columns + FP4_TILE_COLUMNS - 1) / FP4_TILE_COLUMNS, passes = (columns + FP4_COLUMNS - 1) / FP4_COLUMNS;
+    int64_t pages = v.batch.table_pages;
+    if (window) pages = std::min(pages, (int64_t(window) + FP4_TILE_COLUMNS + sinks) / FP4_PAGE + 3);
+    const int64_t tile_groups = tiles * v.H * batch;
+    a.width = 11 * tiles < 2 * passes && (tile_groups >= 384 || (tile_groups >= 16 && pages >= 256)) ? FP4_TILE_COLUMNS : FP4_COLUMNS;
     a.blocks = int((columns + a.width - 1) / a.width);
     a.rows = int(std::min<int64_t>(columns, a.width));
     // Steps that a block of columns can have.
     const int unit = a.width == FP4_TILE_COLUMNS ? FP4_PAGE : FP4_STEP;
-    int64_t most = int64_t(v.batch.table_pages) * (FP4_PAGE / unit);
-    if (window) most = std::min(most, (int64_t(window) + a.width + sinks) / unit + 3);
-    const int batch = v.batch.batch;
+    const int64_t most = pages * (FP4_PAGE / unit);
     const int64_t streams = int64_t(a.blocks) * v.H, room = FP4_PART_ROWS / a.rows / streams;   // workgroups that the workspace takes
-    a.least_steps = streams * batch * (most / FP4_LEAST_STEPS) <= FP4_FEW_GROUPS ? FP4_LEAST_STEPS : FP4_MORE_STEPS;
+    a.least_steps = a.width == FP4_TILE_COLUMNS ? FP4_LEAST_PAGES : streams * batch * (most / FP4_LEAST_STEPS) <= FP4_FEW_GROUPS ? FP4_LEAST_STEPS : FP4_MORE_STEPS;
     const int64_t useful = (most + a.least_steps - 1) / a.least_steps;       // splits of a sequence
     const int chunk = std::min(batch, FP4_FLAT), chunks = (batch + FP4_FLAT - 1) / FP4_FLAT;
     const int64_t want = FP4_GROUPS / streams, more = FP4_MORE_GROUPS / streams;

@@ -269,3 +269,13 @@ def test_joined_by_the_last_workgroup_and_by_a_kernel(G):
     """Splits of one sequence: few rows (joined where they are made) and many."""
     for lens in ([1200], [20000]):
         run(lens, [1], 1, G, 128 if G < 4 else 64, torch.float16, seed=G)
+
+
+@pytest.mark.parametrize("D, H, G, lens, new, window, sinks", [
+    (128, 12, 4, [600] * 8, [150, 300, 160, 1, 20, 600, 31, 0], 0, 0), (64, 16, 3, [500, 300, 900] * 5, [200, 170, 130] * 5, 0, 0),
+    (64, 24, 1, [1200] * 4, [1000, 100, 513, 1200], 300, 70), (128, 8, 16, [400] * 4, [400, 64, 399, 10], 33, 5),
+    (64, 4, 4, [17000, 16500], [70, 130], 0, 0), (128, 3, 8, [20000], [100], 0, 0), (128, 16, 5, [333] * 8, [333] * 8, 1, 0)])
+def test_many_rows(D, H, G, lens, new, window, sinks):
+    """The kernel for many rows: blocks of 128 columns, full and ragged, split contexts, windows that end inside a page."""
+    run(lens, new, H, G, D, torch.float16, window, sinks, seed=H)
+    run(lens[:4], new[:4], H, G, D, torch.bfloat16, window, sinks, seed=H + 1, out_dtype=torch.float32)
