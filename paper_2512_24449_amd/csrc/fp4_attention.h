@@ -201,20 +201,21 @@ template <int HD>
 struct Fp4Column {
     static constexpr int OT = HD / 16;
     float4_t o[OT];
-    float l, m, bar, lift;   // sum of this lane's weights; what the weights are relative to; score that moves it; P_LIFT - m * scale
-    int hi, lo;              // last token that the column sees; first of its window
+    float l, m, lift;        // sum of this lane's weights; what the weights are relative to; P_LIFT - m * scale
+    int hi;                  // last token that the column sees
 
     __device__ inline void clear() {
 #pragma unroll
         for (int i = 0; i < OT; ++i) o[i] = float4_t{0, 0, 0, 0};
         l = 0.0f;
-        m = bar = -INFINITY;
+        m = -INFINITY;
         lift = P_LIFT;
     }
     // Scores of T / 2 times eight tokens, the first from t8 on, the next 32 further: those that the column does not see count
     // nothing.
     template <int T>
-    __device__ inline void mask(float4_t (&s)[T], int t8, int end, int sinks) const {
+    __device__ inline void mask(float4_t (&s)[T], int t8, int end, int window, int sinks) const {
+        const int lo = window ? hi - window + 1 : 0;
 #pragma unroll
         for (int i = 0; i < 4 * T; ++i) {
             const int t = t8 + 32 * (i >> 3) + (i & 7);
@@ -227,6 +228,7 @@ struct Fp4Column {
         float top = fmaxf(s[0][0], s[0][1]);
 #pragma unroll
         for (int i = 1; i < 2 * T; ++i) top = max3(top, s[i >> 1][2 * (i & 1)], s[i >> 1][2 * (i & 1) + 1]);
+        const float bar = m + scale.slack;
         if (__any(top > bar)) {
             top = column_max(top);
             if (top > bar) {
@@ -235,7 +237,6 @@ struct Fp4Column {
                 for (int i = 0; i < OT; ++i) o[i] *= f;
                 l *= f;
                 m = top;
-                bar = top + scale.slack;
                 lift = P_LIFT - top * scale.scale;
             }
         }

@@ -53,7 +53,7 @@ struct Fp4Pages {
 };
 
 template <int HD, bool BF16>
-__global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(Fp4Attention a) {
+__global__ __launch_bounds__(256, HD == 128 ? 3 : 4) void fp4_attention_kernel(Fp4Attention a) {
     using P = Fp4Block<HD>;
     constexpr int KW = HD / 32, VH = HD / 64, OT = HD / 16;
     __shared__ float lds_o[4][FP4_COLUMNS][HD + 4];
@@ -78,7 +78,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(F
     const int64_t out_row = seq.first + row;
     const bool real = column < columns && out_row >= 0 && out_row < v.n_rows;
     Fp4Column<HD> col;
-    col.hi = max(seq.pos0 + row, -1), col.lo = a.window ? col.hi - a.window + 1 : 0;
+    col.hi = max(seq.pos0 + row, -1);
     const Fp4Scale scale(a.scale);
     uint4_t q[KW];
 #pragma unroll
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(F
         for (int x = 0; x < VH; ++x) vs[x] = from.vs[x];
         if (from.t0 + FP4_STEP > min(from.end, first_hi + 1) || from.t0 < last_lo) {   // (wave-uniform)
             const int t8 = from.t0 + 8 * g;
-            col.mask(s, t8, from.end, a.sinks);
+            col.mask(s, t8, from.end, a.window, a.sinks);
 #pragma unroll
             for (int x = 0; x < VH; ++x) vs[x] = seen_scales(vs[x], t8, steps.begin, from.end, a.sinks);
         }

@@ -92,7 +92,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : 3) void fp4_tile_kernel(Fp4Att
         const int column = column0 + 16 * (NB * wave + n) + c16, row = column / v.G, head = h * v.G + column % v.G;
         const int64_t out_row = seq.first + row;
         const bool real = column < columns && out_row >= 0 && out_row < v.n_rows;
-        col[n].hi = max(seq.pos0 + row, -1), col[n].lo = a.window ? col[n].hi - a.window + 1 : 0;
+        col[n].hi = max(seq.pos0 + row, -1);
         col[n].clear();
 #pragma unroll
         for (int i = 0; i < KW; ++i) {
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : 3) void fp4_tile_kernel(Fp4Att
             static_assert(OT == 2 * KW, "as many operands of V for 32 tokens as of K");
             if (t0 + FP4_PAGE > min(end, first_hi + 1) || t0 < last_lo) {
 #pragma unroll
-                for (int n = 0; n < NB; ++n) col[n].mask(s[n], t0 + 8 * g, end, a.sinks);
+                for (int n = 0; n < NB; ++n) col[n].mask(s[n], t0 + 8 * g, end, a.window, a.sinks);
             }
             uint4_t p[NB][2];
 #pragma unroll
