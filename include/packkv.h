@@ -465,7 +465,7 @@ int kv_fp4_read(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, void *k, voi
  * sees nothing becomes zeros (lse: -infinity).
  * q: device [n_rows][H_q][D] of `type` (fp16 or bf16), rows q_stride elements apart (a
  * multiple of 8, at least H_q * D), 16-byte aligned; out: device [n_rows][H_q][D]
- * contiguous of `out_type` (any), 16-byte aligned; lse: null, or device fp32
+ * contiguous of `out_type` (any), 16-byte aligned, not overlapping q; lse: null, or device fp32
  * [n_rows][H_q], the natural logarithm of the softmax's sum (with the scores' maximum
  * in it), for joining this result with one over other tokens.  Rows of no sequence are
  * left as they were.

@@ -468,10 +468,15 @@ class FP4Batch:
         self.table_pages = int(table_pages)
         if not (0 <= self.max_new < 2 ** 31 and 1 <= self.table_pages < 2 ** 31):
             _refuse(what, "max_new is 0 or more, table_pages 1 or more")
-        self.lens, self.new_rows, self.first_row, self.page_table = lens, new_rows, first_row, page_table
+        self._tensors = (lens, new_rows, first_row, page_table)   # whose addresses the structure holds
         self._c = kv_fp4_batch_t(self.batch, self.max_new, self.table_pages,
                                  *(None if t is None else t.data_ptr() for t in (lens, new_rows, first_row, page_table)))
         self._ref, self._address, self._on = C.byref(self._c), C.addressof(self._c), self.device.index
+
+    lens = property(lambda self: self._tensors[0])
+    new_rows = property(lambda self: self._tensors[1])
+    first_row = property(lambda self: self._tensors[2])
+    page_table = property(lambda self: self._tensors[3])
 
 
 class FP4KVCache:

@@ -373,7 +373,7 @@ int launch_fp4_attention(const kv_fp4_cache *c, const Fp4View &v, const void *q,
     const int64_t useful = (most + a.least_steps - 1) / a.least_steps;       // splits of a sequence
     const int chunk = std::min(batch, FP4_FLAT), chunks = (batch + FP4_FLAT - 1) / FP4_FLAT;
     const int64_t want = FP4_GROUPS / streams, more = FP4_MORE_GROUPS / streams;
-    a.flat = batch > 1 && useful > 1 && room >= 2 * chunk * chunks;
+    a.flat = batch > 1 && useful > 1 && room > 2 * chunk * chunks;   // (the workgroups are below 2^16 then)
     if (a.flat) {
         a.splits = int(std::min({std::max<int64_t>(more / chunks, 2 * chunk), chunk * (1 + useful), room / chunks}));
         a.few = int(std::max<int64_t>(want / chunks - chunk, 1));

@@ -279,3 +279,35 @@ def test_many_rows(D, H, G, lens, new, window, sinks):
     """The kernel for many rows: blocks of 128 columns, full and ragged, split contexts, windows that end inside a page."""
     run(lens, new, H, G, D, torch.float16, window, sinks, seed=H)
     run(lens[:4], new[:4], H, G, D, torch.bfloat16, window, sinks, seed=H + 1, out_dtype=torch.float32)
+
+
+def test_padded_batch():
+    """Rows at b * max_new, fewer than max_new of some sequences: the others are left as they were."""
+    lens, new, most = [70, 200, 9], [3, 5, 0], 6
+    cache, k, v, table = filled(lens, 2, 4, 64, torch.float16)
+    q = rows(18, 4, 64, torch.float16, 4)
+    batch = binding.FP4Batch(ints(lens), most, table, new_rows=ints(new))
+    out, lse = torch.full((18, 4, 64), 7.0, dtype=torch.float16, device=DEV), torch.full((18, 4), 7.0, device=DEV)
+    cache.kv_fp4_attention(q.to(DEV).view(3, 6, 4, 64), batch, 0.1, out=out.view(3, 6, 4, 64), lse=lse.view(3, 6, 4))
+    which = torch.tensor([0, 1, 2, 6, 7, 8, 9, 10])
+    check(cache, k, v, lens, new, q[which], out[which.to(DEV)], lse[which.to(DEV)], 0.1)
+    left = [i for i in range(18) if i not in which.tolist()]
+    assert bool((out[left] == 7.0).all()) and bool((lse[left] == 7.0).all())
+
+
+@pytest.mark.parametrize("batch", [1025, 32768, 33000])
+def test_thousands_of_sequences(batch):
+    """As many sequences in one call give what they give a thousand at a time."""
+    lens = torch.randint(0, 65, (batch,), generator=torch.Generator().manual_seed(1), dtype=torch.int32).to(DEV)
+    cache = binding.FP4KVCache(batch, 1, 2, 64)
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    k, v = (torch.randn(64 * batch, 1, 64, generator=gen, device=DEV).half() for _ in range(2))
+    q = torch.randn(batch, 2, 64, generator=gen, device=DEV).half()
+    table = torch.randperm(batch, generator=torch.Generator().manual_seed(3), dtype=torch.int32).view(-1, 1).to(DEV)
+    first = 64 * torch.arange(batch, dtype=torch.int32, device=DEV)
+    cache.kv_fp4_append(k, v, binding.FP4Batch(lens, 64, table, new_rows=lens, first_row=first))
+    out = cache.kv_fp4_attention(q, binding.FP4Batch(lens, 1, table), 0.125)
+    for at in range(0, batch, 1000):
+        part = cache.kv_fp4_attention(q[at:at + 1000], binding.FP4Batch(lens[at:at + 1000], 1, table[at:at + 1000]), 0.125)
+        assert torch.equal(part, out[at:at + 1000])
+    assert not out[lens == 0].any() and bool(torch.isfinite(out).all()) and bool(out[lens > 0].any(2).all())
