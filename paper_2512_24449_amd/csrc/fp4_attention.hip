@@ -334,16 +334,18 @@ int launch_fp4_clear(const kv_fp4_cache *c, hipStream_t s) {
 // streaming kernel, heads of 128 (64): 16 sequences of 2000 tokens, 32 kv-heads, 64 columns each 104 / 79 us (85 / 49), 96 columns
 // 81 / 103 (59 / 64), 128 columns 86 / 133 (61 / 83); 64 of 4000 tokens, 8 kv-heads, 96 columns 141 / 188 (102 / 118); one of
 // 30000, 8 kv-heads, 256 columns 60 / 70 (43 / 46); one of 2000, 8 kv-heads, 512 columns 31 / 16 (27 / 12).
-// Workgroups that a call is split into: not quite two to each of the 256 compute units (a third one on some of them would hold
-// up the call), or more than fit at once (those end at different times, so that no compute unit is left without) where
-// that leaves FP4_LONG_STEPS to each.  Four sequences of up to 32788 tokens, 8 kv-heads: 480 workgroups 26.9 us, 512 28.3, 256
-// 27.1, 768 29.
-constexpr int64_t FP4_GROUPS = 480, FP4_MORE_GROUPS = 1536;
+//
+// Workgroups that a call is split into: one to each of the 256 compute units, or, where that leaves more than FP4_LONG_STEPS to
+// each, more than fit at once (those end at different times, so that no compute unit is left without).  Passes with 256 /
+// 480: 32 heads x 4100 tokens 13.0 / 13.6 us, four sequences of up to 32788 tokens, 8 kv-heads, 27.4 / 27.7, three of 21683, two
+// kv-heads, 12.1 / 13.0, one of 103991, 8 kv-heads, 20.7 / 19.9; with 1536 where splits are long: 156 (sequence, head) pairs of up
+// to 69824 tokens 217 / 238.
+constexpr int64_t FP4_GROUPS = 256, FP4_MORE_GROUPS = 1536;
 // The last workgroup of a sequence joins its splits itself where twice its fair share of them makes so many rows of partial
-// results at most (it has no more then); beyond, a kernel with a
-// workgroup to each row of the output does.  Passes joined so / by the kernel: one head x 1000 tokens 7.8 / 8.6 us, a window
-// of 4096 of 8 kv-heads in 11 splits 9.6 / 10.6, four sequences of up to 32788 28.3 / 29, 32 heads x 4100 in 11 splits 13.2 /
-// 13.0; where no sequence turns out to be split (8 sequences x 52 heads) the kernel would be launched for nothing.
+// results at most (it has no more then); beyond, a kernel does, a workgroup to each row of the output.  Passes joined so / by
+// the kernel: one head x 1000 tokens 8.0 / 9.5 us, a window of 4096 of 8 kv-heads in 11 splits 9.9 / 11.2, four sequences of up
+// to 32788 27.4 / 29.1, 32 heads x 4100 in 8 splits 13.0 / 12.8; where no sequence turns out to be split (8 sequences x 52 heads)
+// the kernel would be launched for nothing.
 constexpr int64_t FP4_MERGED_ROWS = 256;
 
 int launch_fp4_attention(const kv_fp4_cache *c, const Fp4View &v, const void *q, int64_t q_stride, bool bf16, float sm_scale,
