@@ -72,7 +72,7 @@ struct Fp4Attention {
     }
 };
 
-// Four words of a row (32 values' codes, HD / 4 of a lane) as operands: value pairs in the order of the channels.
+// A word of a row of K (eight channels of a token) as an operand.
 template <bool BF16>
 __device__ inline uint4_t row_operand(uint32_t w, float scale) {
     if constexpr (BF16)
