@@ -134,10 +134,10 @@ __device__ inline float column_sum(float x) {
     return __uint_as_float(a) + __uint_as_float(b);
 }
 
-__device__ inline float max3(float a, float b, float c) {   // (without the instructions that quiet a signalling NaN first)
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-    return r;
+// The largest of three, a NaN if one is: one instruction, and the compiler's own, so that it waits for the matrix products whose
+// results these are (inline assembly would read them whenever it comes).  fmaxf would quiet signalling NaNs first.
+__device__ inline float max3(float a, float b, float c) {
+    return __builtin_elementwise_maximum(a, __builtin_elementwise_maximum(b, c));
 }
 
 // exp2(a - b) where -inf - -inf means no weight.
