@@ -469,7 +469,8 @@ int kv_fp4_read(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, void *k, voi
  * [n_rows][H_q], the natural logarithm of the softmax's sum (with the scores' maximum
  * in it), for joining this result with one over other tokens.  Rows of no sequence are
  * left as they were.
- * q.Khat: exact products on the matrix cores, fp32 sums; softmax in fp32; its weights
+ * q.Khat: exact products on the matrix cores, fp32 sums; softmax in fp32, of differences to the row's
+ * largest score (which may be as large as fp32 holds); its weights
  * enter the product with Vhat as fp16 (scaled by a power of two: a relative error of
  * at most 2^-11 down to 2^-26 of the row's largest weight), sums in fp32.  A NaN or
  * infinity in q stays with its row and head.  Sums have a fixed order: the result

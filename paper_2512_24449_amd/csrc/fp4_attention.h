@@ -11,6 +11,7 @@
 #pragma once
 
 #include <algorithm>
+#include <cfloat>
 
 #include "fp4.h"
 #include "last_group.h"
@@ -32,6 +33,10 @@ constexpr int FP4_TILE_COLUMNS = 128;    // of a block of the tile kernel, whose
 // scale no sums then.  They are held as 2^P_LIFT times their size, so that the largest is between 2^12 and 2^15, and fp16
 // keeps its eleven bits down to 2^-26 of it.
 constexpr float P_LIFT = 12.0f, P_SLACK = 3.0f;
+// How the maximum m is subtracted: up to |m * scale| of P_FAR in the exponential's argument, one instruction to a score,
+// s * scale + (P_LIFT - m * scale), whose bracket is rounded to 2^-13 at most; beyond, where that rounding would come to be whole powers
+// of two, from the score: (s - m) * scale + P_LIFT, for the waves that have such a column.
+constexpr float P_FAR = 2048.0f;
 // The workspace: a counter byte for each of so many (stream, sequence) pairs whose splits are joined by the last workgroup
 // of them, and partial results, at most so many rows (of a column in a split) of HD + 4 floats.
 constexpr int FP4_COUNTERS = 4096;
@@ -137,15 +142,15 @@ __device__ inline float column_sum(float x) {
 // The largest of three, a NaN if one is: one instruction, and the compiler's own, so that it waits for the matrix products whose
 // results these are (inline assembly would read them whenever it comes).  fmaxf would quiet signalling NaNs first.
 __device__ inline float max3(float a, float b, float c) {
-    return __builtin_elementwise_maximum(a, __builtin_elementwise_maximum(b, c));
+    return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
 }
 
-// exp2(a - b) where -inf - -inf means no weight.
-__device__ inline float weight_of(float a, float b) { return b == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(a - b); }
+// The weight of a maximum a relative to b; -inf relative to -inf: none.
+__device__ inline float weight_of(float a, float b, float scale) { return b == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((a - b) * scale); }
 
 // The natural logarithm of a sum of weights l (2^P_LIFT times their size) relative to the maximum m.
-__device__ inline float log_sum(float m, float l) {
-    return l > 0.0f || l != l ? (m - P_LIFT + __log2f(l)) * 0.6931471805599453f : -INFINITY;
+__device__ inline float log_sum(float m, float l, float scale) {
+    return l > 0.0f || l != l ? (m * scale - P_LIFT + __log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
 template <int N>
@@ -201,16 +206,19 @@ template <int HD>
 struct Fp4Column {
     static constexpr int OT = HD / 16;
     float4_t o[OT];
-    float l, m, lift;        // sum of this lane's weights; what the weights are relative to; P_LIFT - m * scale
+    float l;                 // sum of this lane's weights
+    // The score that the weights are relative to, and P_LIFT less it times the scale.  Beyond P_FAR, and before the first score, m is
+    // -inf, so that every score seen is above it, and `lift` the score.
+    float m, lift;
     int hi;                  // last token that the column sees
 
     __device__ inline void clear() {
 #pragma unroll
         for (int i = 0; i < OT; ++i) o[i] = float4_t{0, 0, 0, 0};
         l = 0.0f;
-        m = -INFINITY;
-        lift = P_LIFT;
+        m = lift = -INFINITY;
     }
+    __device__ inline float largest() const { return m == -INFINITY ? lift : m; }
     // Scores of T / 2 times eight tokens, the first from t8 on, the next 32 further: those that the column does not see count
     // nothing.
     template <int T>
@@ -224,31 +232,39 @@ struct Fp4Column {
     }
     // The tokens' weights as operands.
     template <int T>
-    __device__ inline void weigh(const float4_t (&s)[T], const Fp4Scale &scale, uint4_t (&p)[T / 2]) {
-        float top = fmaxf(s[0][0], s[0][1]);
+    __device__ inline void weigh(float4_t (&s)[T], const Fp4Scale &scale, uint4_t (&p)[T / 2]) {
+        float top = max3(s[0][0], s[0][1], s[0][2]);
 #pragma unroll
-        for (int i = 1; i < 2 * T; ++i) top = max3(top, s[i >> 1][2 * (i & 1)], s[i >> 1][2 * (i & 1) + 1]);
-        const float bar = m + scale.slack;
-        if (__any(top > bar)) {
+        for (int i = 3; i + 1 < 4 * T; i += 2) top = max3(top, s[i >> 2][i & 3], s[(i + 1) >> 2][(i + 1) & 3]);
+        top = __builtin_elementwise_maximum(top, s[T - 1][3]);
+        float add = lift;
+        if (__any(top - m > scale.slack)) {
             top = column_max(top);
-            if (top > bar) {
-                const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - top) * scale.scale);
+            float now = largest();
+            if (top - now > scale.slack) {
+                const float f = now == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((now - top) * scale.scale);
 #pragma unroll
                 for (int i = 0; i < OT; ++i) o[i] *= f;
                 l *= f;
-                m = top;
-                lift = P_LIFT - top * scale.scale;
+                now = top;
+            }
+            m = now, add = lift = fmaf(-now, scale.scale, P_LIFT);
+            const bool far = !(fabsf(lift) <= P_FAR);   // (of the column: others of the wave weigh as they would without it)
+            if (__builtin_expect(__any(far), false)) {
+                const float base = far ? fmaxf(now, -FLT_MAX) : 0.0f;   // (no score so far: nothing to subtract)
+#pragma unroll
+                for (int i = 0; i < T; ++i) s[i] -= base;
+                if (far) m = -INFINITY, lift = now, add = P_LIFT;
             }
         }
 #pragma unroll
         for (int i = 0; i < 2 * T; ++i) {
-            const float x = __builtin_amdgcn_exp2f(fmaf(s[i >> 1][2 * (i & 1)], scale.scale, lift));
-            const float y = __builtin_amdgcn_exp2f(fmaf(s[i >> 1][2 * (i & 1) + 1], scale.scale, lift));
+            const float x = __builtin_amdgcn_exp2f(fmaf(s[i >> 1][2 * (i & 1)], scale.scale, add));
+            const float y = __builtin_amdgcn_exp2f(fmaf(s[i >> 1][2 * (i & 1) + 1], scale.scale, add));
             l += x + y;
             p[i >> 2][i & 3] = __builtin_bit_cast(uint32_t, half2_t{_Float16(x), _Float16(y)});
         }
     }
-    __device__ inline float scaled_max(const Fp4Scale &scale) const { return m == -INFINITY ? m : m * scale.scale; }
 };
 
 // Scales (a byte each) of the lane's eight tokens: of one that no row sees, which may be any bits, 0 -- no infinity times a weight

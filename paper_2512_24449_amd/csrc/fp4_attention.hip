@@ -56,8 +56,9 @@ struct Fp4Pages {
     __device__ inline int at(int i) const { return __builtin_amdgcn_readlane(page, i); }
 };
 
+// (heads of 64: 96 registers, one more would cost the fifth wave of a SIMD)
 template <int HD, bool BF16>
-__global__ __launch_bounds__(256, HD == 128 ? 3 : 4) void fp4_attention_kernel(Fp4Attention a) {
+__global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(Fp4Attention a) {
     using P = Fp4Block<HD>;
     constexpr int KW = HD / 32, VH = HD / 64, OT = HD / 16;
     __shared__ float lds_o[4][FP4_COLUMNS][HD + 4];
@@ -148,14 +149,14 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 4) void fp4_attention_kernel(F
         }
     }
     float4_t(&o)[OT] = col.o;
-    const float l = column_sum(col.l), m = col.scaled_max(scale);
+    const float l = column_sum(col.l), m = col.largest();
 
     // The four waves' results: each scaled to their common maximum, then summed.  A lane's o[4x + c][i] is channel
     // 64x + 16g + 4i + c.
     if (g == 0) lds_m[wave][c16] = m, lds_l[wave][c16] = l;
     __syncthreads();
     const float top = fmaxf(fmaxf(lds_m[0][c16], lds_m[1][c16]), fmaxf(lds_m[2][c16], lds_m[3][c16]));
-    const float mine = weight_of(m, top);
+    const float mine = weight_of(m, top, scale.scale);
 #pragma unroll
     for (int x = 0; x < VH; ++x)
 #pragma unroll
@@ -169,7 +170,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 4) void fp4_attention_kernel(F
     const float to_m = fmaxf(fmaxf(lds_m[0][to], lds_m[1][to]), fmaxf(lds_m[2][to], lds_m[3][to]));
     float to_l = 0.0f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) to_l += lds_l[w][to] * weight_of(lds_m[w][to], to_m);
+    for (int w = 0; w < 4; ++w) to_l += lds_l[w][to] * weight_of(lds_m[w][to], to_m, scale.scale);
     const auto place = [&](int column, int64_t &index) {   // of a column's output row; false: it has none
         const int64_t out = seq.first + column / v.G;
         index = out * (int64_t(v.H) * v.G) + h * v.G + column % v.G;
@@ -199,7 +200,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 4) void fp4_attention_kernel(F
         }
         if (part == 0) {
             if (share.splits == 1) {
-                if (a.lse) a.lse[index] = log_sum(to_m, to_l);
+                if (a.lse) a.lse[index] = log_sum(to_m, to_l, scale.scale);
             } else if (a.counters) {
                 store_shared(row + HD, to_m, to_l);
             } else {
@@ -230,7 +231,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 4) void fp4_attention_kernel(F
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if (s0 + i * each >= share.splits) break;
-                const float now = fmaxf(m, ml[i].x), old = weight_of(m, now), f = weight_of(ml[i].x, now);
+                const float now = fmaxf(m, ml[i].x), old = weight_of(m, now, scale.scale), f = weight_of(ml[i].x, now, scale.scale);
                 m = now;
                 l = l * old + ml[i].y * f;
                 r[0] = r[0] * old + x[i].x * f, r[1] = r[1] * old + x[i].y * f;
@@ -246,7 +247,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 4) void fp4_attention_kernel(F
             for (int i = 1; i < each; ++i) {
                 const float *from = mine + i * (HD + 4);
                 const float4 x = *reinterpret_cast<const float4 *>(from + 4 * four);
-                const float now = fmaxf(m, from[HD]), old = weight_of(m, now), f = weight_of(from[HD], now);
+                const float now = fmaxf(m, from[HD]), old = weight_of(m, now, scale.scale), f = weight_of(from[HD], now, scale.scale);
                 m = now;
                 l = l * old + from[HD + 1] * f;
                 r[0] = r[0] * old + x.x * f, r[1] = r[1] * old + x.y * f, r[2] = r[2] * old + x.z * f, r[3] = r[3] * old + x.w * f;
@@ -257,7 +258,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 4) void fp4_attention_kernel(F
 #pragma unroll
         for (int i = 0; i < 4; ++i) r[i] *= inverse;
         store_out(a.out, a.out_type, index * HD + 4 * four, r);
-        if (a.lse && four == 0) a.lse[index] = log_sum(m, l);
+        if (a.lse && four == 0) a.lse[index] = log_sum(m, l, scale.scale);
     }
 }
 
@@ -292,7 +293,8 @@ __global__ __launch_bounds__(256) void fp4_join_kernel(Fp4Attention a) {
     if (lane == 0) shared[wave] = m;
     __syncthreads();
     m = fmaxf(fmaxf(shared[0], shared[1]), fmaxf(shared[2], shared[3]));
-    const float f = weight_of(my_m, m);
+    const Fp4Scale scale(a.scale);
+    const float f = weight_of(my_m, m, scale.scale);
     weight[s] = f;
     float l = my_l * f;
 #pragma unroll
@@ -320,7 +322,7 @@ __global__ __launch_bounds__(256) void fp4_join_kernel(Fp4Attention a) {
     if (a.out_type == KV_TYPE_FP32) static_cast<float *>(a.out)[at] = r;
     else if (a.out_type == KV_TYPE_BF16) static_cast<__bf16 *>(a.out)[at] = __bf16(r);
     else static_cast<_Float16 *>(a.out)[at] = _Float16(r);
-    if (a.lse && threadIdx.x == 0) a.lse[index] = log_sum(m, l);
+    if (a.lse && threadIdx.x == 0) a.lse[index] = log_sum(m, l, scale.scale);
 }
 
 __global__ __launch_bounds__(64) void fp4_clear_kernel(uint32_t *counters) {

@@ -189,7 +189,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : 3) void fp4_tile_kernel(Fp4Att
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
         const int column = column0 + 16 * (NB * wave + n) + c16;
-        const float l = column_sum(col[n].l), m = col[n].scaled_max(scale);
+        const float l = column_sum(col[n].l), m = col[n].largest();
         const int64_t out_row = seq.first + column / v.G, index = out_row * (int64_t(v.H) * v.G) + h * v.G + column % v.G;
         if (column >= columns || out_row < 0 || out_row >= v.n_rows) continue;
         float *row = a.part + (a.part_row(stream, share.b, share.first, column - column0) + int64_t(share.split) * a.rows) * (HD + 4);
@@ -204,7 +204,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : 3) void fp4_tile_kernel(Fp4Att
         }
         if (g == 0) {
             if (share.splits > 1) row[HD] = m, row[HD + 1] = l;
-            else if (a.lse) a.lse[index] = log_sum(m, l);
+            else if (a.lse) a.lse[index] = log_sum(m, l, scale.scale);
         }
     }
 }
