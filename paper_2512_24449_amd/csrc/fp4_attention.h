@@ -12,6 +12,7 @@
 
 #include <algorithm>
 #include <cfloat>
+#include <cmath>
 
 #include "fp4.h"
 #include "last_group.h"
@@ -52,11 +53,33 @@ constexpr int FP4_LEAST_PAGES = 4;       // the same, of the tile kernel
 // Steps of a split that more workgroups than fit at once may have: then its start costs little.
 constexpr int FP4_LONG_STEPS = 64;
 
+// sm_scale * log2(e) as the kernels use it.  A negative scale is one of -q: the largest scaled score is then that of the
+// largest score.  With 0 all tokens that are seen weigh the same: q is taken as 0 then and the scale as 1 (0 times -infinity, the
+// score of a token that is not seen, would be a NaN), a NaN or an infinity in q as the NaN that 0 times it is.
+struct Fp4Scale {
+    float scale, slack;      // slack: P_SLACK / scale
+    uint32_t sign;           // of two fp16 or bf16 values of q
+    bool zero;
+    static Fp4Scale of(float s) {
+        const float size = s == 0.0f ? 1.0f : std::fabs(s);
+        return {size, std::fmin(P_SLACK / size, FLT_MAX), s < 0.0f ? 0x80008000u : 0u, s == 0.0f};
+    }
+    // Eight values of q, times 0.
+    template <bool BF16>
+    static __device__ inline uint4_t nothing(uint4_t x) {
+        constexpr uint32_t INFINITE = BF16 ? 0x7F80u : 0x7C00u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            x[i] = ((x[i] & 0x7FFFu) >= INFINITE ? 0x7FFFu : 0u) | (((x[i] >> 16) & 0x7FFFu) >= INFINITE ? 0x7FFF0000u : 0u);
+        return x;
+    }
+};
+
 struct Fp4Attention {
     Fp4View v;
     const uint16_t *q;
     int64_t q_stride;
-    float scale;             // sm_scale * log2(e)
+    Fp4Scale scale;
     int window, sinks;
     void *out;
     int out_type;
@@ -190,15 +213,6 @@ struct Fp4Steps {
         n = end > 0 && first_row < rows ? sink_steps + max((end + UNIT - 1) / UNIT - window_step, 0) : 0;
     }
     __device__ inline int token(int step) const { return UNIT * (step < sink_steps ? step : step - sink_steps + window_step); }
-};
-
-// sm_scale * log2(e) as the kernels use it.  A negative scale is one of -q: the largest scaled score is then that of the
-// largest score.  Scores are below 2^39, so below 1e-30 all that are seen weigh the same, as with 0 (which would make a NaN of a
-// score that is not seen).
-struct Fp4Scale {
-    float scale, slack;      // slack: P_SLACK / scale
-    uint32_t sign;           // of two fp16 or bf16 values of q
-    __device__ inline explicit Fp4Scale(float s) : scale(fmaxf(fabsf(s), 1e-30f)), sign(s < 0.0f ? 0x80008000u : 0u) { slack = P_SLACK / scale; }
 };
 
 // A column of a wave's matrix products: its running softmax and its sums.

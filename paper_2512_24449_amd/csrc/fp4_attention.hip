@@ -84,12 +84,16 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(F
     const bool real = column < columns && out_row >= 0 && out_row < v.n_rows;
     Fp4Column<HD> col;
     col.hi = max(seq.pos0 + row, -1);
-    const Fp4Scale scale(a.scale);
+    const Fp4Scale &scale = a.scale;
     uint4_t q[KW];
 #pragma unroll
     for (int i = 0; i < KW; ++i) {
         q[i] = uint4_t{0, 0, 0, 0};
         if (real) q[i] = *reinterpret_cast<const uint4_t *>(a.q + out_row * a.q_stride + int64_t(head) * HD + g * (HD / 4) + 8 * i) ^ scale.sign;
+    }
+    if (scale.zero) {
+#pragma unroll
+        for (int i = 0; i < KW; ++i) q[i] = Fp4Scale::nothing<BF16>(q[i]);
     }
     col.clear();
     // a step whose tokens every column of the block sees needs no masks
@@ -293,8 +297,7 @@ __global__ __launch_bounds__(256) void fp4_join_kernel(Fp4Attention a) {
     if (lane == 0) shared[wave] = m;
     __syncthreads();
     m = fmaxf(fmaxf(shared[0], shared[1]), fmaxf(shared[2], shared[3]));
-    const Fp4Scale scale(a.scale);
-    const float f = weight_of(my_m, m, scale.scale);
+    const float scale = a.scale.scale, f = weight_of(my_m, m, scale);
     weight[s] = f;
     float l = my_l * f;
 #pragma unroll
@@ -322,7 +325,7 @@ __global__ __launch_bounds__(256) void fp4_join_kernel(Fp4Attention a) {
     if (a.out_type == KV_TYPE_FP32) static_cast<float *>(a.out)[at] = r;
     else if (a.out_type == KV_TYPE_BF16) static_cast<__bf16 *>(a.out)[at] = __bf16(r);
     else static_cast<_Float16 *>(a.out)[at] = _Float16(r);
-    if (a.lse && threadIdx.x == 0) a.lse[index] = log_sum(m, l, scale.scale);
+    if (a.lse && threadIdx.x == 0) a.lse[index] = log_sum(m, l, scale);
 }
 
 __global__ __launch_bounds__(64) void fp4_clear_kernel(uint32_t *counters) {
@@ -362,7 +365,7 @@ int launch_fp4_attention(const kv_fp4_cache *c, const Fp4View &v, const void *q,
     a.v = v;
     a.q = static_cast<const uint16_t *>(q);
     a.q_stride = q_stride;
-    a.scale = sm_scale * 1.4426950408889634f;
+    a.scale = Fp4Scale::of(sm_scale * 1.4426950408889634f);
     a.window = window, a.sinks = sinks;
     a.out = out, a.out_type = out_type, a.lse = lse;
     const int batch = v.batch.batch;

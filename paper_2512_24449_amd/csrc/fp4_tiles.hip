@@ -89,7 +89,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : 3) void fp4_tile_kernel(Fp4Att
     const int per_split = (steps.n + share.splits - 1) / share.splits;
     const int step0 = share.split * per_split, step_end = min(step0 + per_split, steps.n);
 
-    const Fp4Scale scale(a.scale);
+    const Fp4Scale &scale = a.scale;
     Fp4Column<HD> col[NB];
     uint4_t q[NB][KW];
 #pragma unroll
@@ -103,6 +103,10 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : 3) void fp4_tile_kernel(Fp4Att
         for (int i = 0; i < KW; ++i) {
             q[n][i] = uint4_t{0, 0, 0, 0};
             if (real) q[n][i] = *reinterpret_cast<const uint4_t *>(a.q + out_row * a.q_stride + int64_t(head) * HD + g * (HD / 4) + 8 * i) ^ scale.sign;
+        }
+        if (scale.zero) {
+#pragma unroll
+            for (int i = 0; i < KW; ++i) q[n][i] = Fp4Scale::nothing<BF16>(q[n][i]);
         }
     }
     // what the wave's columns see: from the first row's window (or the first tokens) to the last row
