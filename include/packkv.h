@@ -462,7 +462,8 @@ int kv_fp4_read(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, void *k, voi
  * over the tokens t that the row at position p sees: t <= p, and with window > 0 also
  * t > p - window or t < sinks (the first tokens stay visible).  window = 0: no
  * window.  Tokens that no row sees are not read: their pages may be missing.  A row that
- * sees nothing becomes zeros (lse: -infinity).  sm_scale: finite; with 0 all tokens that a row sees weigh the same.
+ * sees nothing becomes zeros (lse: -infinity).  sm_scale: below 2.3e38 in size
+ * (sm_scale * log2(e) is finite in fp32); with 0 all tokens that a row sees weigh the same.
  * q: device [n_rows][H_q][D] of `type` (fp16 or bf16), rows q_stride elements apart (a
  * multiple of 8, at least H_q * D), 16-byte aligned; out: device [n_rows][H_q][D]
  * contiguous of `out_type` (any), 16-byte aligned, not overlapping q; lse: null, or device fp32

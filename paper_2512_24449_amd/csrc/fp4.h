@@ -19,6 +19,7 @@ struct kv_fp4_cache {
 namespace packkv {
 
 constexpr int FP4_PAGE = KV_FP4_PAGE_TOKENS, FP4_GROUP = KV_FP4_GROUP;
+constexpr float FP4_LOG2E = 1.4426950408889634f;              // scores are scaled for powers of two
 constexpr int FP4_E_LEAST = 127 - 23, FP4_E_MOST = 127 + 13;  // as held: e + 127
 
 // Offsets inside a head's block of a page.

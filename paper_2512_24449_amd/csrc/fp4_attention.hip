@@ -365,7 +365,7 @@ int launch_fp4_attention(const kv_fp4_cache *c, const Fp4View &v, const void *q,
     a.v = v;
     a.q = static_cast<const uint16_t *>(q);
     a.q_stride = q_stride;
-    a.scale = Fp4Scale::of(sm_scale * 1.4426950408889634f);
+    a.scale = Fp4Scale::of(sm_scale * FP4_LOG2E);
     a.window = window, a.sinks = sinks;
     a.out = out, a.out_type = out_type, a.lse = lse;
     const int batch = v.batch.batch;

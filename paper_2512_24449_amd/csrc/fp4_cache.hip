@@ -392,7 +392,7 @@ extern "C" int kv_fp4_attention(kv_fp4_cache_t *c, const kv_fp4_batch_t *batch, 
     if (rc) return rc;
     if (n_rows < 0 || (type != KV_TYPE_FP16 && type != KV_TYPE_BF16) || out_type < KV_TYPE_FP16 || out_type > KV_TYPE_FP32)
         return KV_ERR_ARG;
-    if (!std::isfinite(sm_scale) || window < 0 || sinks < 0) return KV_ERR_ARG;
+    if (!std::isfinite(sm_scale * FP4_LOG2E) || window < 0 || sinks < 0) return KV_ERR_ARG;
     if (q_stride < int64_t(c->cfg.n_q_heads) * c->cfg.head_dim || q_stride % 8) return KV_ERR_ARG;
     if (n_rows == 0 || batch->max_new == 0) return KV_OK;
     if (!aligned(q, 16) || !aligned(out, 16) || (lse && !aligned(lse, 4))) return KV_ERR_ARG;
