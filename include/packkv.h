@@ -416,7 +416,8 @@ typedef struct {
  * memory.  Rows outside the tensors are left out. */
 typedef struct {
     int32_t batch;             /* sequences, 1 .. 65535                           */
-    int32_t max_new;           /* most new rows of a sequence; new_rows above it count as it */
+    int32_t max_new;           /* most new rows of a sequence; new_rows above it count as it.  append and read take
+                                  max_new * n_kv_heads * head_dim below 2^37, attention max_new * n_q_heads / n_kv_heads up to 2^22 */
     int32_t table_pages;       /* pages of a sequence at most: 1 .. 2^24          */
     const int32_t *lens;       /* [batch], negative: 0                            */
     const int32_t *new_rows;   /* [batch]; null: max_new of every sequence        */

@@ -248,11 +248,14 @@ __global__ __launch_bounds__(256) void fp4_read_kernel(Fp4View v, uint8_t *__res
 // Tiles of `tokens` tokens that a sequence's new rows can touch, wherever they begin.
 inline int tiles_touched(int max_new, int tokens) { return int((int64_t(max_new) + tokens - 2) / tokens) + 1; }
 
+// Workgroups of 256 threads along an axis: a launch takes fewer than 2^32 threads.
+constexpr int64_t FP4_GROUPS_MOST = (int64_t(1) << 24) - 1;
+
 int launch_fp4_append(const kv_fp4_cache *c, const Fp4View &v, const void *k, int64_t k_stride, const void *vv, int64_t v_stride,
                       bool bf16, hipStream_t s) {
     const int tiles = tiles_touched(v.batch.max_new, c->cfg.head_dim == 128 ? Fp4Tile<128>::TOKENS : Fp4Tile<64>::TOKENS);
     const int64_t groups = (int64_t(tiles) * v.H + 3) / 4;
-    if (groups > 0x1FFFFFFF) return KV_ERR_UNSUPPORTED;
+    if (groups > FP4_GROUPS_MOST) return KV_ERR_UNSUPPORTED;
     const dim3 grid = dim3(uint32_t(groups), uint32_t(v.batch.batch));
 #define LAUNCH(HD, BF)                                                                                                    \
     hipLaunchKernelGGL((fp4_append_kernel<HD, BF>), grid, dim3(256), 0, s, v, static_cast<const uint16_t *>(k), \
@@ -270,7 +273,7 @@ int launch_fp4_append(const kv_fp4_cache *c, const Fp4View &v, const void *k, in
 int launch_fp4_read(const kv_fp4_cache *c, const Fp4View &v, void *k, void *vv, int type, hipStream_t s) {
     const int tiles = tiles_touched(v.batch.max_new, c->cfg.head_dim == 128 ? Fp4Tile<128>::TOKENS : Fp4Tile<64>::TOKENS);
     const int64_t groups = (int64_t(tiles) * v.H + 3) / 4;
-    if (groups > 0x1FFFFFFF) return KV_ERR_UNSUPPORTED;
+    if (groups > FP4_GROUPS_MOST) return KV_ERR_UNSUPPORTED;
     const dim3 grid = dim3(uint32_t(groups), uint32_t(v.batch.batch));
 #define LAUNCH(HD, TYPE)                                                                                                  \
     hipLaunchKernelGGL((fp4_read_kernel<HD, TYPE>), grid, dim3(256), 0, s, v, static_cast<uint8_t *>(k), \
