@@ -481,7 +481,13 @@ class FP4Batch:
 
 class FP4KVCache:
     """A 4-bit paged cache (packkv.h: MXFP4 rows in pages of 64 tokens): owns the pages and the workspace (torch tensors)
-    and the kv_fp4_cache_t handle.  Which pages a sequence has, and how long it is, is the program's (FP4Batch)."""
+    and the kv_fp4_cache_t handle.  Which pages a sequence has, and how long it is, is the program's (FP4Batch).
+
+    Calls run on torch's current stream, or on `stream` (a torch stream, or a hipStream_t as int).  On another stream than the current
+    one the program sees to the order, as with torch's own operators: that stream waits for what made the inputs, and whoever reads
+    the outputs for it.  Tensors of such a call may be dropped as soon as it returns: their memory is not reused before that stream is done.
+    Calls on the current stream record nothing: a program that makes another stream current for some of them keeps the cache, and
+    tensors made on other streams, until that one is done."""
 
     def __init__(self, n_pages, n_kv_heads, n_q_heads, head_dim=HEAD_DIM, device="cuda:0"):
         self.cfg = kv_fp4_config_t(n_kv_heads, n_q_heads, head_dim, n_pages)
@@ -542,12 +548,24 @@ class FP4KVCache:
         if rc != KV_OK:
             _check(rc, what)
 
-    def _used_on(self, stream, *tensors):
-        """Tensors made here are used on `stream`, which need not be the one they were made on."""
+    def _stream(self, stream):
+        return torch.cuda.ExternalStream(stream, device=self.device) if isinstance(stream, int) else stream
+
+    def _new(self, shape, dtype, stream):
+        """An output, in memory that the stream which writes it may write at once; the current stream is taken to read it."""
+        if stream is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(stream):
+            made = torch.empty(shape, dtype=dtype, device=self.device)
+        made.record_stream(torch.cuda.current_stream(self.device))
+        return made
+
+    def _keep(self, stream, batch, *tensors):
+        """What a call on `stream` uses is not reused before `stream` is done with it, even if the program drops it now."""
         if stream is not None:
-            on = torch.cuda.ExternalStream(stream, device=self.device) if isinstance(stream, int) else stream
-            for t in tensors:
-                t.record_stream(on)
+            for t in (*tensors, *batch._tensors, self.pages, self.workspace):
+                if t is not None:
+                    t.record_stream(stream)
 
     def kv_fp4_append(self, k, v, batch, stream=None):
         """k, v: fp16 or bf16 [rows, H_kv, D] (or [batch, n, H_kv, D]); may be parts of wider rows."""
@@ -560,6 +578,7 @@ class FP4KVCache:
             _refuse("kv_fp4_append", "k and v of as many rows and of one type")
         self._call("kv_fp4_append", _lib.kv_fp4_append, batch, stream, k.data_ptr(), k_stride, v.data_ptr(), v_stride,
                    _TYPES[k.dtype], rows)
+        self._keep(self._stream(stream), batch, k, v)
 
     def kv_fp4_read(self, batch, n_rows, dtype=torch.float16, k=None, v=None, stream=None):
         """The batch's new rows as the cache holds them: (k, v), [n_rows, H_kv, D] of dtype; rows of no sequence are not written."""
@@ -570,12 +589,13 @@ class FP4KVCache:
         what, shape = "kv_fp4_read", (n_rows, self.n_kv_heads, self.head_dim)
         if dtype not in _TYPES:
             _refuse(what, "dtype is float16, bfloat16 or float32")
-        made = [torch.empty(shape, dtype=dtype, device=self.device) if t is None else t for t in (k, v)]
+        on = self._stream(stream)
+        made = [self._new(shape, dtype, on) if t is None else t for t in (k, v)]
         for t in made:
             if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != self.device:
                 _refuse(what, "k and v are contiguous %s %s on %s" % (shape, dtype, self.device))
         self._call(what, _lib.kv_fp4_read, batch, stream, made[0].data_ptr(), made[1].data_ptr(), _TYPES[dtype], n_rows)
-        self._used_on(stream, *made)
+        self._keep(on, batch, *made)
         return tuple(made)
 
     def kv_fp4_attention(self, q, batch, sm_scale, window=0, sinks=0, out=None, lse=None, stream=None):
@@ -587,8 +607,9 @@ class FP4KVCache:
                 return done
         what = "kv_fp4_attention"
         rows, q_stride = self._rows(what, q, self.n_q_heads, (torch.float16, torch.bfloat16))
+        on = self._stream(stream)
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
+            out = self._new(q.shape, q.dtype, on)
         elif out.dtype not in _TYPES or out.shape != q.shape or not out.is_contiguous() or out.device != self.device:
             _refuse(what, "out is contiguous, of q's shape and on its device")
         if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:-1] or not lse.is_contiguous() or
@@ -598,7 +619,7 @@ class FP4KVCache:
             _refuse(what, "window and sinks are 0 or more")
         self._call(what, _lib.kv_fp4_attention, batch, stream, q.data_ptr(), q_stride, _TYPES[q.dtype], rows, sm_scale,
                    window, sinks, out.data_ptr(), _TYPES[out.dtype], None if lse is None else lse.data_ptr())
-        self._used_on(stream, out)
+        self._keep(on, batch, q, out, lse)
         return out
 
 
