@@ -446,33 +446,38 @@ class FP4Batch:
     are rows first_row[b], first_row[b] + 1, ... of the call's tensors.  lens, new_rows, first_row: int32 device tensors
     [batch]; page_table: int32 [batch, pages of a sequence at most].  Without new_rows every sequence has max_new of them, without first_row
     sequence b's begin at row b * max_new, without page_table sequence b has pages b * table_pages .. of the cache.
-    The tensors are kept and read when a call's kernels run: a program changes their contents from step to step."""
+    The tensors are kept and read when a call's kernels run: a program changes their contents from step to step.
+    What the batch was made of stays: its attributes are read-only."""
 
     def __init__(self, lens, max_new, page_table=None, new_rows=None, first_row=None, table_pages=None):
         what = "FP4Batch"
         if lens.dim() != 1 or lens.shape[0] < 1:
             _refuse(what, "lens is [batch]")
-        self.batch, self.max_new, self.device = lens.shape[0], int(max_new), lens.device
+        batch, max_new, device = lens.shape[0], int(max_new), lens.device
         for name, t in (("lens", lens), ("new_rows", new_rows), ("first_row", first_row)):
-            if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != (self.batch,) or not t.is_contiguous()):
+            if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != (batch,) or not t.is_contiguous()):
                 _refuse(what, "%s is int32 [batch], contiguous" % name)
         if page_table is not None:
-            if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.shape[0] != self.batch or \
+            if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.shape[0] != batch or \
                     not page_table.is_contiguous() or table_pages not in (None, page_table.shape[1]):
                 _refuse(what, "page_table is int32 [batch, table_pages], contiguous")
             table_pages = page_table.shape[1]
         elif table_pages is None:
             _refuse(what, "page_table or table_pages")
-        if any(t is not None and t.device != self.device for t in (new_rows, first_row, page_table)):
+        if any(t is not None and t.device != device for t in (new_rows, first_row, page_table)):
             _refuse(what, "tensors of one device")
-        self.table_pages = int(table_pages)
-        if not (0 <= self.max_new < 2 ** 31 and 1 <= self.table_pages < 2 ** 31):
+        table_pages = int(table_pages)
+        if not (0 <= max_new < 2 ** 31 and 1 <= table_pages < 2 ** 31):
             _refuse(what, "max_new is 0 or more, table_pages 1 or more")
         self._tensors = (lens, new_rows, first_row, page_table)   # whose addresses the structure holds
-        self._c = kv_fp4_batch_t(self.batch, self.max_new, self.table_pages,
+        self._c = kv_fp4_batch_t(batch, max_new, table_pages,
                                  *(None if t is None else t.data_ptr() for t in (lens, new_rows, first_row, page_table)))
-        self._ref, self._address, self._on = C.byref(self._c), C.addressof(self._c), self.device.index
+        self._ref, self._address, self._on = C.byref(self._c), C.addressof(self._c), device.index
 
+    batch = property(lambda self: self._c.batch)
+    max_new = property(lambda self: self._c.max_new)
+    table_pages = property(lambda self: self._c.table_pages)
+    device = property(lambda self: self._tensors[0].device)
     lens = property(lambda self: self._tensors[0])
     new_rows = property(lambda self: self._tensors[1])
     first_row = property(lambda self: self._tensors[2])
