@@ -488,6 +488,8 @@ class FP4KVCache:
     """A 4-bit paged cache (packkv.h: MXFP4 rows in pages of 64 tokens): owns the pages and the workspace (torch tensors)
     and the kv_fp4_cache_t handle.  Which pages a sequence has, and how long it is, is the program's (FP4Batch).
 
+    There is no backward pass: results carry no gradient, whatever k, v and q require.
+
     Calls run on torch's current stream, or on `stream` (a torch stream, or a hipStream_t as int).  On another stream than the current
     one the program sees to the order, as with torch's own operators: that stream waits for what made the inputs, and whoever reads
     the outputs for it.  Tensors of such a call may be dropped as soon as it returns: their memory is not reused before that stream is done.

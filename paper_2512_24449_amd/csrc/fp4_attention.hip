@@ -1,8 +1,8 @@
 // Attention over the 4-bit paged cache for few new rows: a wave streams the cache past 16 columns, 32 tokens a step, the next
 // step's rows on their way into registers while one is computed.  Four waves of a workgroup take every fourth step and join
 // their sums through LDS.  Long contexts are bound by the rate at which HBM delivers pages (8 sequences x 52 heads x 32000 tokens,
-// 1.81 GB, in 312 us: 5.8 TB/s where a plain read reaches 6.8), with heads of 64 by vector instructions as well (130 a step of 2176
-// bytes, 180 a step of 4352 with heads of 128; 96 pairs of sequence and head of 111355 tokens 155 us, 4.7 TB/s), short ones by
+// 1.81 GB, in 313 us: 5.8 TB/s where a plain read reaches 6.8), with heads of 64 by vector instructions as well (130 a step of 2176
+// bytes, 180 a step of 4352 with heads of 128; 8 sequences x 12 heads x 111355 tokens, 0.73 GB, 143 us, 5.1 TB/s), short ones by
 // a chain of memory latencies -- lengths, page numbers, rows, partial results -- of some 5 us.
 #include "fp4_attention.h"
 

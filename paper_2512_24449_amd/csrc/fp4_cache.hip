@@ -20,7 +20,8 @@ typedef uint16_t ushort2_t __attribute__((ext_vector_type(2)));
 // quad of lanes, and the 8 x 8 codes that V's layout turns around are the lane's own.  Neighbouring waves take neighbouring
 // heads of the same tokens, which lie next to each other in the rows.  Measured, heads of 128: 8 sequences x
 // 52 heads x 32000 tokens written in 1.68 ms (8.6 GB moved, 5.1 TB/s), 25077 bf16 rows of 32 heads written in 124 us
-// (4.2 TB/s) and read back in 96 (5.4), 131072 rows of 8 heads read back in 145 us (4.7 TB/s; a copy of 4 GiB reaches 4.7 here).
+// (4.2 TB/s) and read back in 96 (5.4), 131072 rows of 8 heads read back in 145 us (4.7 TB/s): of the same
+// kind as a copy, which reaches 4.7 to 5.0 here, reading and writing as much; reads alone reach 6.8, writes alone 6.9.
 template <int HD>
 struct Fp4Tile {
     static constexpr int ROW_LANES = HD / 8, TOKENS = 8 * 64 / ROW_LANES;

@@ -4,10 +4,10 @@
 // kilobyte in a row, without bank conflicts.  Two tiles in turn, one barrier each: while one is multiplied, the next is converted
 // and the one after that is on its way.
 //
-// Bound by the vector instructions of the softmax and by the matrix cores, which share the issue: per 32 columns and page 244
+// Bound by the vector instructions of the softmax and by the matrix cores, which share the issue: per 32 columns and page 232
 // vector instructions (68 of them the conversion, 32 exponentials) and 64 products of 16 cycles; a product keeps vector instructions out
-// for about 8.  2048 rows of 32 heads at 12288 (4.5e11 operations) take 442 us, 1010 TFLOP/s, where a large library product reaches
-// 1100; the matrix cores are busy 40 % of the time, two waves to a SIMD.
+// for about 8.  2048 rows of 32 heads at 12288 (4.5e11 operations) take 446 us, 1000 TFLOP/s, where a large library product reaches
+// 1345 once its clock is up; the matrix cores are busy 39 % of the time, two waves to a SIMD.
 #include "fp4_attention.h"
 
 namespace packkv {
