@@ -475,7 +475,7 @@ int kv_fp4_read(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, void *k, voi
  * largest score (which may be as large as fp32 holds); its weights
  * enter the product with Vhat as fp16 (scaled by a power of two: a relative error of
  * at most 2^-11 down to 2^-26 of the row's largest weight), sums in fp32.  A NaN or
- * infinity in q stays with its row and head.  Sums have a fixed order: the result
+ * infinity in q makes its row and head NaN where it sees a token, and no other.  Sums have a fixed order: the result
  * is bitwise reproducible.  Uses the workspace: attention calls on one cache must not overlap.
  */
 int kv_fp4_attention(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, const void *q, int64_t q_stride, int32_t type,

@@ -30,6 +30,12 @@ struct Fp4Block {
 };
 inline size_t fp4_block_bytes(int head_dim) { return size_t(FP4_PAGE) * (head_dim + head_dim / 16); }
 
+// The larger of each of two unsigned 16-bit numbers.
+typedef uint16_t ushort2_t __attribute__((ext_vector_type(2)));
+__device__ inline uint32_t max16(uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2_t, a), __builtin_bit_cast(ushort2_t, b)));
+}
+
 // What a kernel needs to know of the cache and the batch.
 struct Fp4View {
     uint8_t *pages;

@@ -55,7 +55,7 @@ constexpr int FP4_LONG_STEPS = 64;
 
 // sm_scale * log2(e) as the kernels use it.  A negative scale is one of -q: the largest scaled score is then that of the
 // largest score.  With 0 all tokens that are seen weigh the same: q is taken as 0 then and the scale as 1 (0 times -infinity, the
-// score of a token that is not seen, would be a NaN), a NaN or an infinity in q as the NaN that 0 times it is.
+// score of a token that is not seen, would be a NaN).
 struct Fp4Scale {
     float scale, slack;      // slack: P_SLACK / scale
     uint32_t sign;           // of two fp16 or bf16 values of q
@@ -64,14 +64,21 @@ struct Fp4Scale {
         const float size = s == 0.0f ? 1.0f : std::fabs(s);
         return {size, std::fmin(P_SLACK / size, FLT_MAX), s < 0.0f ? 0x80008000u : 0u, s == 0.0f};
     }
-    // Eight values of q, times 0.
-    template <bool BF16>
-    static __device__ inline uint4_t nothing(uint4_t x) {
+    // q as an operand, but for its sign: an infinity as the NaN that it makes of its row (whose scores may all be -infinity, and are
+    // then told from those of a row that sees nothing), and what is finite as 0 where the scale is.
+    template <bool BF16, int N>
+    __device__ inline void settle(uint4_t (&q)[N]) const {
         constexpr uint32_t INFINITE = BF16 ? 0x7F80u : 0x7C00u;
+        uint32_t m = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            x[i] = ((x[i] & 0x7FFFu) >= INFINITE ? 0x7FFFu : 0u) | (((x[i] >> 16) & 0x7FFFu) >= INFINITE ? 0x7FFF0000u : 0u);
-        return x;
+        for (int i = 0; i < 4 * N; ++i) m = max16(m, q[i / 4][i % 4] & 0x7FFF7FFFu);
+        if (__builtin_expect(!zero && !__any(max(m & 0xFFFFu, m >> 16) >= INFINITE), true)) return;
+#pragma unroll
+        for (int i = 0; i < 4 * N; ++i) {
+            const uint32_t x = q[i / 4][i % 4], finite = zero ? 0u : x;
+            q[i / 4][i % 4] = ((x & 0x7FFFu) >= INFINITE ? 0x7FFFu : finite & 0xFFFFu) |
+                              (((x >> 16) & 0x7FFFu) >= INFINITE ? 0x7FFF0000u : finite & 0xFFFF0000u);
+        }
     }
 };
 

@@ -91,10 +91,6 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(F
         q[i] = uint4_t{0, 0, 0, 0};
         if (real) q[i] = *reinterpret_cast<const uint4_t *>(a.q + out_row * a.q_stride + int64_t(head) * HD + g * (HD / 4) + 8 * i) ^ scale.sign;
     }
-    if (scale.zero) {
-#pragma unroll
-        for (int i = 0; i < KW; ++i) q[i] = Fp4Scale::nothing<BF16>(q[i]);
-    }
     col.clear();
     // a step whose tokens every column of the block sees needs no masks
     const int first_hi = max(seq.pos0 + steps.first_row, -1), last_lo = a.window ? max(seq.pos0 + steps.last_row - a.window + 1, 0) : 0;
@@ -144,6 +140,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 3 : 5) void fp4_attention_kernel(F
         // Every fetch is made, behind the last one of that step again: a transfer that is made on some paths only would have
         // the next use of any wait for all of them.
         fetch(in[0], step);
+        scale.settle<BF16>(q);      // (here, where it waits for nothing that the transfers do not)
         for (int at = step; at < last; at += 8) {
             fetch(in[1], min(at + 4, most));
             compute(in[0]);

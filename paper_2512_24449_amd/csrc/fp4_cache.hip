@@ -12,7 +12,6 @@ namespace packkv {
 typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf162_t __attribute__((ext_vector_type(2)));
 typedef float float2_t __attribute__((ext_vector_type(2)));
-typedef uint16_t ushort2_t __attribute__((ext_vector_type(2)));
 
 // Both kernels move bytes: what bounds them is HBM (and, for a few tokens, three dependent memory latencies: lengths, page
 // number, rows).  They give a wave a tile of 8 * 512 / HD tokens (an aligned eight per row of HD / 8 lanes) of one sequence and
@@ -48,10 +47,6 @@ __device__ inline void turn_nibbles(uint32_t (&w)[8]) {
         w[j] = (a & m) | ((b & m) << 4);
         w[j + 1] = ((a >> 4) & m) | (b & ~m);
     }
-}
-
-__device__ inline uint32_t max16(uint32_t a, uint32_t b) {
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2_t, a), __builtin_bit_cast(ushort2_t, b)));
 }
 
 // Eight channels of a token (two to a word, fp16 or bf16) -> their codes; the byte of the scale is found over the quad of

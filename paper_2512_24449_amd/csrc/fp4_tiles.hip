@@ -104,10 +104,6 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : 3) void fp4_tile_kernel(Fp4Att
             q[n][i] = uint4_t{0, 0, 0, 0};
             if (real) q[n][i] = *reinterpret_cast<const uint4_t *>(a.q + out_row * a.q_stride + int64_t(head) * HD + g * (HD / 4) + 8 * i) ^ scale.sign;
         }
-        if (scale.zero) {
-#pragma unroll
-            for (int i = 0; i < KW; ++i) q[n][i] = Fp4Scale::nothing<BF16>(q[n][i]);
-        }
     }
     // what the wave's columns see: from the first row's window (or the first tokens) to the last row
     const int wave0 = column0 + 16 * NB * wave, wave_columns = min(columns - wave0, 16 * NB);
@@ -134,6 +130,8 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : 3) void fp4_tile_kernel(Fp4Att
         convert(0);
         t0 = in.t0, end = in.end;
         fetch(min(step0 + 1, step_end - 1));
+#pragma unroll
+        for (int n = 0; n < NB; ++n) scale.settle<BF16>(q[n]);
         __syncthreads();
     }
     for (int step = step0; step < step_end; ++step) {
