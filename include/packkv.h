@@ -482,6 +482,73 @@ int kv_fp4_attention(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, const v
                      int64_t n_rows, float sm_scale, int32_t window, int32_t sinks, void *out, int32_t out_type,
                      float *lse, void *hip_stream);
 
+/*
+ * The attention weight that every cached token gets from the batch's new rows:
+ *   mass[b][h][t] = past[b][h][t] + sum over the rows that see t and the heads hq of h of
+ *                                   exp(sm_scale * q[row][hq] . Khat[t][h] - lse[row][hq])
+ * with q, sm_scale, window, sinks (and so which rows see t) and lse as the call of kv_fp4_attention on the same batch had or
+ * gave them.  mass: device fp32 [batch][H_kv][mass_tokens]; written are the places of the tokens that the sequence holds
+ * (and the page table and mass have room for), others are left as they were.  past: null (0), or of mass's
+ * size, mass itself or not overlapping it; it is not read for the call's own tokens, positions from lens - new_rows on, which
+ * no earlier row has seen.  A token that no row sees, and one of a missing page, keeps past's.  max_new may be 0: mass is then past.
+ * fp32 throughout, q.Khat as in attention; what lse is off by (a few 2^-24 of its size) is a factor of a row's weights.  A row whose lse is
+ * -infinity gives nothing, one whose q or lse is NaN makes the tokens that it sees NaN.  Sums have a fixed order.  Does not use the
+ * workspace.
+ */
+int kv_fp4_weights(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, const void *q, int64_t q_stride, int32_t type,
+                   int64_t n_rows, float sm_scale, int32_t window, int32_t sinks, const float *lse, const float *past,
+                   float *mass, int64_t mass_tokens, void *hip_stream);
+/*
+ * Which tokens a sequence keeps, for every kv-head by itself: all if it holds no more than its budget, else as many as the budget,
+ * namely the first `sinks`, then the last `recent` (as many of both as the budget has room for), then of the others those of the
+ * largest mass, of equal ones the first (0 and -0 are equal, a NaN is above all).  mass as of kv_fp4_weights; tokens from mass_tokens on have
+ * 0.  budgets: device int32 [batch], or null: keep of each; a budget above keep (1 or more) is keep, below 0 it is 0.
+ * kept: device int32 [batch][H_kv][keep], the positions in ascending order, -1 behind them; n_kept: device int32 [batch],
+ * how many: the least of lens, the table's room and the budget.  Of the batch lens and table_pages are used; pages are not read.
+ */
+int kv_fp4_select(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, const float *mass, int64_t mass_tokens, int32_t keep,
+                  const int32_t *budgets, int32_t sinks, int32_t recent, int32_t *kept, int32_t *n_kept, void *hip_stream);
+/*
+ * Moves kept tokens together: token i of (sequence b, kv-head h) of `to` becomes token kept[b][h][i] of `from`, for i below
+ * n_kept[b] (device int32 [batch]; at most keep), bit by bit.  kept: device int32 [batch][H_kv][keep], in any order, a position as
+ * often as one likes; one that the sequence does not hold (lens, room of the table) or whose page is missing becomes a token of zeros.
+ * `to`: as many sequences, and the pages that they go to, which belong to one sequence of the call only and are none that the call reads;
+ * what would go to a page that is missing is left out.  Its lens are not read (they may be n_kept itself: the batch of the sequences
+ * from then on).  In the group of eight tokens that the last one is in, those behind it become zeros.
+ * mass, mass_out: both null, or device fp32 [batch][H_kv][mass_tokens] and, not overlapping, [batch][H_kv][mass_out_tokens]: weights that go with
+ * the tokens (0 of a token that mass has no room for); places from n_kept on are left as they were.
+ * From then on a token's position in the cache is no longer its position in the text: rotary positions of later rows count on
+ * from the text's.
+ */
+int kv_fp4_compact(kv_fp4_cache_t *cache, const kv_fp4_batch_t *from, const kv_fp4_batch_t *to, const int32_t *kept, int32_t keep,
+                   const int32_t *n_kept, const float *mass, int64_t mass_tokens, float *mass_out, int64_t mass_out_tokens,
+                   void *hip_stream);
+
+/* ---- rotary positions -------------------------------------------------------
+ * Of query and key rows, before keys are appended to a cache (of either kind) and queries attend.  For pair i of the first
+ * `dims` channels of a head, channels (x, y) at (i, i + dims / 2), or (2i, 2i + 1) where interleaved, and a row's position p:
+ *     a = 2 pi * p * turns[i] / 2^64
+ *     x' = magnitude * (x cos a - y sin a),  y' = magnitude * (y cos a + x sin a)
+ * Channels from dims on are copied.  Angles are exact to 2^-32 of a turn at any position, sums are fp32, rounded once.
+ */
+typedef struct {
+    int32_t head_dim;      /* even, 2 .. 512                                      */
+    int32_t dims;          /* even, 2 .. head_dim                                 */
+    int32_t interleaved;   /* 0: pairs (i, i + dims / 2)                          */
+    float magnitude;       /* finite                                              */
+    const uint64_t *turns; /* device [dims / 2]: turns that a position makes, in 2^-64 (modulo a turn) */
+} kv_rotary_t;
+/*
+ * positions: device int32 [n_rows], any values, read when the kernel runs.  q: device [n_rows][n_q_heads][head_dim] of `type` (any of the
+ * three), rows q_stride values apart (at least n_q_heads * head_dim), aligned to its type; k likewise, with n_k_heads; either number of heads may be
+ * 0 and its pointers null then.  q_out, k_out: of the same type and shape, the input itself (same stride) or not overlapping any input;
+ * values between rows' ends and the next rows are left as they were.  inverse != 0: the angle's sign is turned (the transpose of the
+ * operation: it takes gradients back, and rows too, with a magnitude of 1).  Rows of 16-byte aligned heads are fastest.
+ */
+int kv_rotary(const kv_rotary_t *rotary, const int32_t *positions, int64_t n_rows, int32_t type, int32_t inverse, const void *q,
+              int64_t q_stride, int32_t n_q_heads, void *q_out, int64_t q_out_stride, const void *k, int64_t k_stride,
+              int32_t n_k_heads, void *k_out, int64_t k_out_stride, void *hip_stream);
+
 /* ---- measurement companions (same shapes, uncompressed fp16 cache) ---------
  * The comparison kernels of Sec. IV-E, hand-written for the same shapes:
  * plain fp16 matrix-vector products over an uncompressed cache stored as

@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes as C
 import importlib.util
+import math
 import os
 import subprocess
 import warnings
@@ -68,6 +69,11 @@ class kv_fp4_sizes_t(C.Structure):
     _fields_ = [("pages", C.c_size_t), ("workspace", C.c_size_t)]
 
 
+class kv_rotary_t(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("dims", C.c_int32), ("interleaved", C.c_int32), ("magnitude", C.c_float),
+                ("turns", C.c_void_p)]
+
+
 class kv_fp4_batch_t(C.Structure):
     _fields_ = [("batch", C.c_int32), ("max_new", C.c_int32), ("table_pages", C.c_int32),
                 ("lens", C.c_void_p), ("new_rows", C.c_void_p), ("first_row", C.c_void_p), ("page_table", C.c_void_p)]
@@ -79,7 +85,7 @@ EXPORTS = ("kv_query_sizes", "kv_cache_create", "kv_cache_destroy", "kv_compress
            "kv_stream_read", "kv_page_pool_state_bytes", "kv_page_pool_create", "kv_page_pool_destroy",
            "kv_page_pool_free_pages", "kv_query_sizes_paged", "kv_cache_create_paged", "kv_cache_release",
            "kv_fp4_query_sizes", "kv_fp4_cache_create", "kv_fp4_cache_destroy", "kv_fp4_append", "kv_fp4_read",
-           "kv_fp4_attention")
+           "kv_fp4_attention", "kv_fp4_weights", "kv_fp4_select", "kv_fp4_compact", "kv_rotary")
 # entry points the native module calls, in its order
 _NATIVE_CALLS = ("kv_compress_append", "kv_compress_append_bf16", "kv_k_matvec", "kv_softmax", "kv_v_matvec",
                  "kv_decode_attention", "kv_cache_restore", "kv_cache_release", "kv_cache_tokens", "kv_fp4_append", "kv_fp4_read",
@@ -168,6 +174,10 @@ def lib():
         L.kv_fp4_append.argtypes = [vp, batch, vp, i64, vp, i64, i32, i64, vp]
         L.kv_fp4_read.argtypes = [vp, batch, vp, vp, i32, i64, vp]
         L.kv_fp4_attention.argtypes = [vp, batch, vp, i64, i32, i64, f32, i32, i32, vp, i32, vp, vp]
+        L.kv_fp4_weights.argtypes = [vp, batch, vp, i64, i32, i64, f32, i32, i32, vp, vp, vp, i64, vp]
+        L.kv_fp4_select.argtypes = [vp, batch, vp, i64, i32, vp, i32, i32, vp, vp, vp]
+        L.kv_fp4_compact.argtypes = [vp, batch, batch, vp, i32, vp, vp, i64, vp, i64, vp]
+        L.kv_rotary.argtypes = [C.POINTER(kv_rotary_t), vp, i64, i32, i32, vp, i64, i32, vp, i64, vp, i64, i32, vp, i64, vp]
         for name in EXPORTS:
             if name not in ("kv_cache_tokens", "kv_strerror", "kv_fp16_v_workspace_bytes",
                             "kv_page_pool_state_bytes"):
@@ -484,7 +494,50 @@ class FP4Batch:
     page_table = property(lambda self: self._tensors[3])
 
 
-class FP4KVCache:
+class _Operators:
+    """What calls on tensors of one device (self.device) have in common."""
+
+    def _row_pitch(self, what, t, heads, dim, types):
+        """Rows and row stride of t: [rows, heads, dim] or [batch, n, heads, dim], the heads of a row next to each other."""
+        if t.device != self.device or t.dtype not in types:
+            _refuse(what, "tensors of %s on %s" % (" or ".join(map(str, types)), self.device))
+        shape, stride = t.shape, t.stride()
+        if t.dim() not in (3, 4) or shape[-2:] != (heads, dim) or \
+                stride[-1] != 1 or (heads > 1 and stride[-2] != dim):
+            _refuse(what, "[rows, %d, %d], the heads of a row next to each other" % (heads, dim))
+        if t.dim() == 3:
+            rows, pitch = shape[0], stride[0]
+        else:
+            rows, pitch = shape[0] * shape[1], stride[1] if shape[1] > 1 else stride[0]
+            if shape[0] > 1 and shape[1] > 1 and stride[0] != shape[1] * stride[1]:
+                _refuse(what, "rows at even distances")
+        return rows, pitch if rows > 1 else heads * dim
+
+    def _made(self, what, function, *args):
+        """function(*args) with the operators' device the current one."""
+        if _current_device is not None and _current_device() == self.device.index:
+            rc = function(*args[:-1], _stream_ptr(args[-1]))
+        else:
+            with torch.cuda.device(self.device):
+                rc = function(*args[:-1], _stream_ptr(args[-1]))
+        if rc != KV_OK:
+            _check(rc, what)
+
+    def _stream(self, stream):
+        return torch.cuda.ExternalStream(stream, device=self.device) if isinstance(stream, int) else stream
+
+    def _new(self, shape, dtype, stream, zeros=False):
+        """An output, in memory that the stream which writes it may write at once; the current stream is taken to read it."""
+        make = torch.zeros if zeros else torch.empty
+        if stream is None:
+            return make(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(stream):
+            made = make(shape, dtype=dtype, device=self.device)
+        made.record_stream(torch.cuda.current_stream(self.device))
+        return made
+
+
+class FP4KVCache(_Operators):
     """A 4-bit paged cache (packkv.h: MXFP4 rows in pages of 64 tokens): owns the pages and the workspace (torch tensors)
     and the kv_fp4_cache_t handle.  Which pages a sequence has, and how long it is, is the program's (FP4Batch).
 
@@ -527,45 +580,22 @@ class FP4KVCache:
             pass
 
     def _rows(self, what, t, heads, types):
-        """Rows and row stride of t: [rows, heads, D] or [batch, n, heads, D], the heads of a row next to each other."""
-        if t.device != self.device or t.dtype not in types:
-            _refuse(what, "tensors of %s on %s" % (" or ".join(map(str, types)), self.device))
-        shape, stride = t.shape, t.stride()
-        if t.dim() not in (3, 4) or shape[-2:] != (heads, self.head_dim) or \
-                stride[-1] != 1 or (heads > 1 and stride[-2] != self.head_dim):
-            _refuse(what, "[rows, %d, %d], the heads of a row next to each other" % (heads, self.head_dim))
-        if t.dim() == 3:
-            rows, pitch = shape[0], stride[0]
-        else:
-            rows, pitch = shape[0] * shape[1], stride[1] if shape[1] > 1 else stride[0]
-            if shape[0] > 1 and shape[1] > 1 and stride[0] != shape[1] * stride[1]:
-                _refuse(what, "rows at even distances")
-        return rows, pitch if rows > 1 else heads * self.head_dim
+        return self._row_pitch(what, t, heads, self.head_dim, types)
 
     def _call(self, what, function, batch, stream, *args):
         if not self.handle:
             _refuse(what, "the cache is closed")
         if batch.device != self.device:
             _refuse(what, "the batch is on %s, the cache on %s" % (batch.device, self.device))
-        if _current_device is not None and _current_device() == self.device.index:
-            rc = function(self.handle, batch._ref, *args, _stream_ptr(stream))
-        else:
-            with torch.cuda.device(self.device):
-                rc = function(self.handle, batch._ref, *args, _stream_ptr(stream))
-        if rc != KV_OK:
-            _check(rc, what)
+        self._made(what, function, self.handle, batch._ref, *args, stream)
 
-    def _stream(self, stream):
-        return torch.cuda.ExternalStream(stream, device=self.device) if isinstance(stream, int) else stream
-
-    def _new(self, shape, dtype, stream):
-        """An output, in memory that the stream which writes it may write at once; the current stream is taken to read it."""
-        if stream is None:
-            return torch.empty(shape, dtype=dtype, device=self.device)
-        with torch.cuda.stream(stream):
-            made = torch.empty(shape, dtype=dtype, device=self.device)
-        made.record_stream(torch.cuda.current_stream(self.device))
-        return made
+    def _plain(self, what, name, t, dtype, shape):
+        """t's address; None: null."""
+        if t is None:
+            return None
+        if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != self.device:
+            _refuse(what, "%s is contiguous %s %s on %s" % (name, dtype, tuple(shape), self.device))
+        return t.data_ptr()
 
     def _keep(self, stream, batch, *tensors):
         """What a call on `stream` uses is not reused before `stream` is done with it, even if the program drops it now."""
@@ -628,6 +658,169 @@ class FP4KVCache:
                    window, sinks, out.data_ptr(), _TYPES[out.dtype], None if lse is None else lse.data_ptr())
         self._keep(on, batch, q, out, lse)
         return out
+
+    def kv_fp4_weights(self, q, lse, batch, sm_scale, window=0, sinks=0, past=None, out=None, stream=None):
+        """The attention weight that every cached token gets from the batch's new rows, on top of `past`: fp32 [batch, H_kv, tokens].
+        q, sm_scale, window and sinks as kv_fp4_attention had them, lse as it gave them; past: null, or of out's shape, or out
+        itself; it counts for the tokens before the new rows.  Without out a new tensor of past's shape, or of the page table's
+        width, zeros where the sequences have no tokens; places of out behind a sequence's tokens are not written."""
+        what, tokens = "kv_fp4_weights", 64 * batch.table_pages
+        rows, q_stride = self._rows(what, q, self.n_q_heads, (torch.float16, torch.bfloat16))
+        on = self._stream(stream)
+        lse_at = self._plain(what, "lse", lse, torch.float32, q.shape[:-1])
+        for t in (past, out):
+            if t is not None:
+                if t.dim() != 3:
+                    _refuse(what, "past and out are [batch, H_kv, tokens]")
+                tokens = t.shape[2]
+        shape = (batch.batch, self.n_kv_heads, tokens)
+        past_at = self._plain(what, "past", past, torch.float32, shape)
+        if not (0 <= window < 2 ** 31 and 0 <= sinks < 2 ** 31):
+            _refuse(what, "window and sinks are 0 or more")
+        if out is None:
+            out = self._new(shape, torch.float32, on, zeros=True)
+        self._call(what, _lib.kv_fp4_weights, batch, stream, q.data_ptr(), q_stride, _TYPES[q.dtype], rows, sm_scale, window, sinks,
+                   lse_at, past_at, self._plain(what, "out", out, torch.float32, shape), tokens)
+        self._keep(on, batch, q, lse, past, out)
+        return out
+
+    def kv_fp4_select(self, mass, batch, keep, sinks=0, recent=0, budgets=None, kept=None, n_kept=None, stream=None):
+        """Which tokens the batch's sequences keep, of mass [batch, H_kv, tokens] (kv_fp4_weights): (kept, n_kept), int32 [batch, H_kv,
+        keep], positions in ascending order and -1 behind them, and int32 [batch].  All of a sequence of no more than keep (or
+        budgets[b], int32 [batch]) tokens; else the first `sinks`, the last `recent` and the others of the largest mass."""
+        what = "kv_fp4_select"
+        keep = int(keep)
+        if mass.dim() != 3 or not (1 <= keep < 2 ** 31 and 0 <= sinks < 2 ** 31 and 0 <= recent < 2 ** 31):
+            _refuse(what, "mass is [batch, H_kv, tokens], keep 1 or more, sinks and recent are 0 or more")
+        tokens, on = mass.shape[2], self._stream(stream)
+        mass_at = self._plain(what, "mass", mass, torch.float32, (batch.batch, self.n_kv_heads, tokens))
+        budgets_at = self._plain(what, "budgets", budgets, torch.int32, (batch.batch,))
+        shape = (batch.batch, self.n_kv_heads, keep)
+        kept = self._new(shape, torch.int32, on) if kept is None else kept
+        n_kept = self._new(shape[:1], torch.int32, on) if n_kept is None else n_kept
+        self._call(what, _lib.kv_fp4_select, batch, stream, mass_at, tokens, keep, budgets_at, sinks, recent,
+                   self._plain(what, "kept", kept, torch.int32, shape), self._plain(what, "n_kept", n_kept, torch.int32, shape[:1]))
+        self._keep(on, batch, mass, budgets, kept, n_kept)
+        return kept, n_kept
+
+    def kv_fp4_compact(self, kept, n_kept, batch, to, mass=None, mass_out=None, stream=None):
+        """Moves the tokens `kept` (int32 [batch, H_kv, keep]; the first n_kept[b], int32 [batch], of each) of batch's sequences together into
+        the pages of `to`, an FP4Batch of as many sequences whose pages the call does not read (its lens may be n_kept).  mass: weights
+        that go with them, [batch, H_kv, tokens], into mass_out, [batch, H_kv, any number] (without it new, [batch, H_kv, keep], zeros
+        behind the kept ones), which is returned."""
+        what, keep = "kv_fp4_compact", kept.shape[-1]
+        shape, on = (batch.batch, self.n_kv_heads, keep), self._stream(stream)
+        kept_at = self._plain(what, "kept", kept, torch.int32, shape)
+        n_at = self._plain(what, "n_kept", n_kept, torch.int32, shape[:1])
+        if to.device != self.device or to.batch != batch.batch:
+            _refuse(what, "both batches are on %s, of as many sequences" % self.device)
+        if any(t is not None and t.dim() != 3 for t in (mass, mass_out)) or (mass is None and mass_out is not None):
+            _refuse(what, "mass and mass_out are [batch, H_kv, tokens]")
+        if mass is not None and mass_out is None:
+            mass_out = self._new(shape, torch.float32, on, zeros=True)
+        sizes = [0 if t is None else t.shape[2] for t in (mass, mass_out)]
+        at = [self._plain(what, name, t, torch.float32, (*shape[:2], n)) for name, t, n in zip(("mass", "mass_out"), (mass, mass_out), sizes)]
+        self._call(what, _lib.kv_fp4_compact, batch, stream, to._ref, kept_at, keep, n_at, at[0], sizes[0], at[1], sizes[1])
+        self._keep(on, batch, kept, n_kept, mass, mass_out, *to._tensors)
+        return mass_out
+
+
+class Rotary(_Operators):
+    """Rotary positions of query and key rows, before keys are appended to a cache and queries attend: the first `dims` channels of a
+    head (all without it) in pairs (i, i + dims / 2), or (2i, 2i + 1) where interleaved, pair i turned by position * f_i.
+
+    f_i = base^(-2i / dims), for contexts of `original` tokens; scaling makes them serve contexts `factor` times as long:
+      "linear"  f_i / factor
+      "base"    the base times factor^(dims / (dims - 2)): the last pair is turned factor times as slowly, the first as before
+      "bands"   f_i / factor of pairs that turn less than `low` times over `original` tokens, f_i from `high` turns on, in between a
+                blend that is linear in the turns
+      "ramp"    f_i / factor of pairs that turn less than `slow` times, f_i of those that do more than `fast` times, in between a blend that is
+                linear in i; the turned channels are multiplied by 0.1 ln(factor) + 1
+    frequencies: all f_i, in radians, instead; magnitude: what the turned channels are multiplied by, instead.
+
+    There is no backward pass; inverse=True is the transposed operation, which takes gradients back.  Streams as of FP4KVCache."""
+
+    def __init__(self, head_dim, dims=None, base=10000.0, interleaved=False, scaling="none", factor=1.0, original=8192, low=1.0, high=4.0,
+                 slow=1.0, fast=32.0, frequencies=None, magnitude=None, device="cuda:0"):
+        what, dims = "Rotary", head_dim if dims is None else dims
+        if head_dim % 2 or dims % 2 or not 2 <= dims <= head_dim:
+            _refuse(what, "head_dim and dims are even, dims 2 .. head_dim")
+        if frequencies is None:
+            frequencies = self._frequencies(what, dims, base, scaling, factor, original, low, high, slow, fast)
+            if magnitude is None:
+                magnitude = 0.1 * math.log(factor) + 1.0 if scaling == "ramp" else 1.0
+        frequencies = [float(f) for f in frequencies]
+        magnitude = 1.0 if magnitude is None else float(magnitude)
+        if len(frequencies) != dims // 2 or not all(map(math.isfinite, [*frequencies, magnitude])):
+            _refuse(what, "dims / 2 finite frequencies, a finite magnitude")
+        # 2^-64 of a turn, modulo a turn, as the signed numbers that torch has
+        turns = [round(math.ldexp(math.fmod(f / (2.0 * math.pi), 1.0), 64)) % 2 ** 64 for f in frequencies]
+        lib()
+        self.head_dim, self.dims, self.interleaved, self.frequencies, self.magnitude = head_dim, dims, bool(interleaved), frequencies, magnitude
+        self._turns = torch.tensor([t - 2 ** 64 if t >= 2 ** 63 else t for t in turns], dtype=torch.int64).to(device)
+        self.device = self._turns.device
+        self._c = kv_rotary_t(head_dim, dims, int(self.interleaved), magnitude, self._turns.data_ptr())
+        self._ref = C.byref(self._c)
+
+    @staticmethod
+    def _frequencies(what, dims, base, scaling, factor, original, low, high, slow, fast):
+        if not (base > 1.0 and factor > 0.0 and original > 0):
+            _refuse(what, "base above 1, factor and original above 0")
+        if scaling == "base":
+            if dims == 2:
+                _refuse(what, 'scaling "base" takes dims of 4 or more')
+            base = base * factor ** (dims / (dims - 2))
+        f = [base ** (-2.0 * i / dims) for i in range(dims // 2)]
+        if scaling == "linear":
+            return [x / factor for x in f]
+        if scaling == "bands":
+            if not 0.0 <= low < high:
+                _refuse(what, "low is below high")
+            own = [min(max((original * x / (2.0 * math.pi) - low) / (high - low), 0.0), 1.0) for x in f]   # what stays of f
+        elif scaling == "ramp":
+            if not 0.0 < slow <= fast:
+                _refuse(what, "slow is at most fast")
+            first, last = (dims * math.log(original / (2.0 * math.pi * turns)) / (2.0 * math.log(base)) for turns in (fast, slow))
+            first, last = max(math.floor(first), 0), min(math.ceil(last), dims - 1)
+            own = [1.0 - min(max((i - first) / max(last - first, 0.001), 0.0), 1.0) for i in range(dims // 2)]
+        elif scaling in ("none", "base"):
+            return f
+        else:
+            _refuse(what, 'scaling is "none", "linear", "base", "bands" or "ramp"')
+        return [x * (w + (1.0 - w) / factor) for x, w in zip(f, own)]
+
+    def kv_rotary(self, q, positions, k=None, out=None, k_out=None, inverse=False, stream=None):
+        """q, k: fp16, bf16 or fp32 [rows, heads, head_dim] (or [batch, n, heads, head_dim]), both of one type; may be parts of wider rows.
+        positions: int32, of q's shape without the last two axes.  Returns what became of q, or of (q, k); out and k_out: where to, which
+        may be q and k themselves.  inverse: turned the other way."""
+        what, types = "kv_rotary", (torch.float16, torch.bfloat16, torch.float32)
+        on, args, kept = self._stream(stream), [], [positions]
+        if positions.dtype != torch.int32 or positions.device != self.device or not positions.is_contiguous() or \
+                positions.shape != q.shape[:-2]:
+            _refuse(what, "positions are contiguous int32 on %s, one to a row of q" % self.device)
+        made = []
+        for t, to in ((q, out), (k, k_out)):
+            if t is None:
+                if to is not None:
+                    _refuse(what, "k_out without k")
+                args += [None, 0, 0, None, 0]
+                continue
+            heads = t.shape[-2] if t.dim() > 2 else 0
+            rows, pitch = self._row_pitch(what, t, heads, self.head_dim, types)
+            if t.dtype != q.dtype or rows != positions.numel():
+                _refuse(what, "q and k of one type, as many rows as positions")
+            to = self._new(t.shape, t.dtype, on) if to is None else to
+            to_rows, to_pitch = self._row_pitch(what, to, heads, self.head_dim, (t.dtype,))
+            if to.shape != t.shape:
+                _refuse(what, "an output is of its input's shape")
+            args += [t.data_ptr(), pitch, heads, to.data_ptr(), to_pitch]
+            made.append(to)
+            kept += [t, to]
+        self._made(what, _lib.kv_rotary, self._ref, positions.data_ptr(), positions.numel(), _TYPES[q.dtype], int(inverse), *args, stream)
+        if on is not None:
+            for t in (*kept, self._turns):
+                t.record_stream(on)
+        return made[0] if k is None else tuple(made)
 
 
 def kv_fp16_k_matvec(k_cache, q, sm_scale, n_kv_heads, scores=None, stream=None):

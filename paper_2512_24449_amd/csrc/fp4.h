@@ -8,6 +8,8 @@
 // eight tokens of a column of V.  Neither is moved between lanes.
 #pragma once
 
+#include <initializer_list>
+
 #include "common.h"
 
 struct kv_fp4_cache {
@@ -44,6 +46,25 @@ struct Fp4View {
     kv_fp4_batch_t batch;
     int64_t n_rows;          // of the call's tensors
 };
+
+// What the entry points have in common.
+inline bool fp4_aligned(const void *p, uintptr_t to) { return p && (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+inline int fp4_check_batch(const kv_fp4_batch_t *b) {
+    if (!b || b->batch < 1 || b->max_new < 0 || !b->lens || b->table_pages < 1) return KV_ERR_ARG;
+    for (const void *p : {static_cast<const void *>(b->lens), static_cast<const void *>(b->new_rows),
+                          static_cast<const void *>(b->first_row), static_cast<const void *>(b->page_table)})
+        if (p && !fp4_aligned(p, 4)) return KV_ERR_ARG;
+    if (b->table_pages > (1 << 24) || b->batch > 65535) return KV_ERR_UNSUPPORTED;
+    return KV_OK;
+}
+
+inline Fp4View fp4_view(const kv_fp4_cache_t *c, const kv_fp4_batch_t *b, int64_t n_rows) {
+    return Fp4View{c->pages, c->cfg.n_pages, c->cfg.n_kv_heads, c->cfg.n_q_heads / c->cfg.n_kv_heads, *b, n_rows};
+}
+
+// Workgroups of 256 threads along an axis: a launch takes fewer than 2^32 threads.
+constexpr int64_t FP4_GROUPS_MOST = (int64_t(1) << 24) - 1;
 
 // A sequence's part of the batch.
 struct Fp4Sequence {

@@ -1,7 +1,6 @@
 // The 4-bit paged cache: host side of its entry points, and the kernels that write rows into pages and read them back.
 // Format and contract are in packkv.h, the reasons for the format in fp4.h.
 #include <cmath>
-#include <initializer_list>
 #include <new>
 
 #include "fp4.h"
@@ -244,9 +243,6 @@ __global__ __launch_bounds__(256) void fp4_read_kernel(Fp4View v, uint8_t *__res
 // Tiles of `tokens` tokens that a sequence's new rows can touch, wherever they begin.
 inline int tiles_touched(int max_new, int tokens) { return int((int64_t(max_new) + tokens - 2) / tokens) + 1; }
 
-// Workgroups of 256 threads along an axis: a launch takes fewer than 2^32 threads.
-constexpr int64_t FP4_GROUPS_MOST = (int64_t(1) << 24) - 1;
-
 int launch_fp4_append(const kv_fp4_cache *c, const Fp4View &v, const void *k, int64_t k_stride, const void *vv, int64_t v_stride,
                       bool bf16, hipStream_t s) {
     const int tiles = tiles_touched(v.batch.max_new, c->cfg.head_dim == 128 ? Fp4Tile<128>::TOKENS : Fp4Tile<64>::TOKENS);
@@ -297,27 +293,12 @@ using namespace packkv;
 
 namespace {
 
-bool aligned(const void *p, uintptr_t to) { return p && (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
-
 int check_config(const kv_fp4_config_t *c) {
     if (!c || c->n_kv_heads < 1 || c->n_q_heads < 1 || c->n_pages < 1 || c->n_pages > 0x7FFFFFFF) return KV_ERR_ARG;
     if (c->n_q_heads % c->n_kv_heads) return KV_ERR_ARG;
     if (c->head_dim != 128 && c->head_dim != 64) return KV_ERR_UNSUPPORTED;
     if (c->n_q_heads > 65535) return KV_ERR_UNSUPPORTED;
     return KV_OK;
-}
-
-int check_batch(const kv_fp4_batch_t *b) {
-    if (!b || b->batch < 1 || b->max_new < 0 || !b->lens || b->table_pages < 1) return KV_ERR_ARG;
-    for (const void *p : {static_cast<const void *>(b->lens), static_cast<const void *>(b->new_rows),
-                          static_cast<const void *>(b->first_row), static_cast<const void *>(b->page_table)})
-        if (p && !aligned(p, 4)) return KV_ERR_ARG;
-    if (b->table_pages > (1 << 24) || b->batch > 65535) return KV_ERR_UNSUPPORTED;
-    return KV_OK;
-}
-
-Fp4View view_of(const kv_fp4_cache_t *c, const kv_fp4_batch_t *b, int64_t n_rows) {
-    return Fp4View{c->pages, c->cfg.n_pages, c->cfg.n_kv_heads, c->cfg.n_q_heads / c->cfg.n_kv_heads, *b, n_rows};
 }
 
 }  // namespace
@@ -338,7 +319,7 @@ extern "C" int kv_fp4_cache_create(const kv_fp4_config_t *cfg, void *pages, void
     kv_fp4_sizes_t need;
     const int rc = kv_fp4_query_sizes(cfg, &need);
     if (rc) return rc;
-    if (!sizes || !out || !aligned(pages, 256) || !aligned(workspace, 256)) return KV_ERR_ARG;
+    if (!sizes || !out || !fp4_aligned(pages, 256) || !fp4_aligned(workspace, 256)) return KV_ERR_ARG;
     if (sizes->pages < need.pages || sizes->workspace < need.workspace) return KV_ERR_ARG;
     kv_fp4_cache *c = new (std::nothrow) kv_fp4_cache;
     if (!c) return KV_ERR_ARG;
@@ -363,38 +344,38 @@ extern "C" int kv_fp4_cache_destroy(kv_fp4_cache_t *cache) {
 
 extern "C" int kv_fp4_append(kv_fp4_cache_t *c, const kv_fp4_batch_t *batch, const void *k, int64_t k_stride, const void *v,
                              int64_t v_stride, int32_t type, int64_t n_rows, void *hip_stream) {
-    const int rc = c ? check_batch(batch) : KV_ERR_ARG;
+    const int rc = c ? fp4_check_batch(batch) : KV_ERR_ARG;
     if (rc) return rc;
     if (n_rows < 0 || (type != KV_TYPE_FP16 && type != KV_TYPE_BF16)) return KV_ERR_ARG;
     const int64_t width = int64_t(c->cfg.n_kv_heads) * c->cfg.head_dim;
     if (k_stride < width || v_stride < width || k_stride % 8 || v_stride % 8) return KV_ERR_ARG;
     if (n_rows == 0 || batch->max_new == 0) return KV_OK;
-    if (!aligned(k, 16) || !aligned(v, 16)) return KV_ERR_ARG;
-    return launch_fp4_append(c, view_of(c, batch, n_rows), k, k_stride, v, v_stride, type == KV_TYPE_BF16,
+    if (!fp4_aligned(k, 16) || !fp4_aligned(v, 16)) return KV_ERR_ARG;
+    return launch_fp4_append(c, fp4_view(c, batch, n_rows), k, k_stride, v, v_stride, type == KV_TYPE_BF16,
                              static_cast<hipStream_t>(hip_stream));
 }
 
 extern "C" int kv_fp4_read(kv_fp4_cache_t *c, const kv_fp4_batch_t *batch, void *k, void *v, int32_t type, int64_t n_rows,
                            void *hip_stream) {
-    const int rc = c ? check_batch(batch) : KV_ERR_ARG;
+    const int rc = c ? fp4_check_batch(batch) : KV_ERR_ARG;
     if (rc) return rc;
     if (n_rows < 0 || type < KV_TYPE_FP16 || type > KV_TYPE_FP32) return KV_ERR_ARG;
     if (n_rows == 0 || batch->max_new == 0) return KV_OK;
-    if ((!k && !v) || (k && !aligned(k, 16)) || (v && !aligned(v, 16))) return KV_ERR_ARG;
-    return launch_fp4_read(c, view_of(c, batch, n_rows), k, v, type, static_cast<hipStream_t>(hip_stream));
+    if ((!k && !v) || (k && !fp4_aligned(k, 16)) || (v && !fp4_aligned(v, 16))) return KV_ERR_ARG;
+    return launch_fp4_read(c, fp4_view(c, batch, n_rows), k, v, type, static_cast<hipStream_t>(hip_stream));
 }
 
 extern "C" int kv_fp4_attention(kv_fp4_cache_t *c, const kv_fp4_batch_t *batch, const void *q, int64_t q_stride, int32_t type,
                                 int64_t n_rows, float sm_scale, int32_t window, int32_t sinks, void *out, int32_t out_type,
                                 float *lse, void *hip_stream) {
-    const int rc = c ? check_batch(batch) : KV_ERR_ARG;
+    const int rc = c ? fp4_check_batch(batch) : KV_ERR_ARG;
     if (rc) return rc;
     if (n_rows < 0 || (type != KV_TYPE_FP16 && type != KV_TYPE_BF16) || out_type < KV_TYPE_FP16 || out_type > KV_TYPE_FP32)
         return KV_ERR_ARG;
     if (!std::isfinite(sm_scale * FP4_LOG2E) || window < 0 || sinks < 0) return KV_ERR_ARG;
     if (q_stride < int64_t(c->cfg.n_q_heads) * c->cfg.head_dim || q_stride % 8) return KV_ERR_ARG;
     if (n_rows == 0 || batch->max_new == 0) return KV_OK;
-    if (!aligned(q, 16) || !aligned(out, 16) || (lse && !aligned(lse, 4))) return KV_ERR_ARG;
-    return launch_fp4_attention(c, view_of(c, batch, n_rows), q, q_stride, type == KV_TYPE_BF16, sm_scale, window, sinks, out,
+    if (!fp4_aligned(q, 16) || !fp4_aligned(out, 16) || (lse && !fp4_aligned(lse, 4))) return KV_ERR_ARG;
+    return launch_fp4_attention(c, fp4_view(c, batch, n_rows), q, q_stride, type == KV_TYPE_BF16, sm_scale, window, sinks, out,
                                 out_type, lse, static_cast<hipStream_t>(hip_stream));
 }

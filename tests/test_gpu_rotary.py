@@ -1,0 +1,167 @@
+"""Rotary positions against 64-bit arithmetic (budget_reference): layouts, parts of a head, types, strides, positions of any size."""
+import pytest
+import torch
+
+from paper_2512_24449_amd import binding
+from tests import budget_reference as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+FAR = 2 ** 31 - 1
+
+
+def rows(n, heads, dim, dtype, seed):
+    return torch.randn(n, heads, dim, generator=torch.Generator().manual_seed(seed)).to(dtype)
+
+
+def check(rotary, got, x, positions, inverse=False):
+    want, bound = ref.turned(x, positions, rotary.frequencies, rotary.magnitude, rotary.interleaved, inverse)
+    bound = ref.rounded(want, bound, x.dtype)
+    off = (got.cpu().double() - want).abs()
+    assert bool((off <= bound).all()), float((off - bound).max())
+    rest = 2 * len(rotary.frequencies)
+    assert torch.equal(got.cpu()[..., rest:], x.cpu()[..., rest:])
+
+
+def positions(n, seed, most=200000):
+    p = torch.randint(0, most, (n,), generator=torch.Generator().manual_seed(seed), dtype=torch.int32)
+    p[:min(n, 4)] = torch.tensor([0, 1, FAR, -7], dtype=torch.int32)[:min(n, 4)]
+    return p
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dim, dims, q_heads, k_heads, n", [
+    (128, 128, 1, 1, 1), (128, 128, 32, 8, 5), (64, 64, 30, 10, 3), (128, 32, 4, 4, 33), (80, 60, 20, 4, 7), (96, 24, 3, 1, 129),
+    (64, 6, 5, 5, 4), (256, 256, 2, 1, 65), (512, 128, 1, 1, 3), (512, 510, 1, 1, 2), (2, 2, 7, 3, 9), (10, 4, 1, 2, 11), (66, 22, 52, 52, 2),
+    (128, 126, 3, 2, 6)])
+def test_layouts_and_types(dim, dims, q_heads, k_heads, n, interleaved, dtype):
+    rotary = binding.Rotary(dim, dims, interleaved=interleaved)
+    q, k, p = rows(n, q_heads, dim, dtype, 1), rows(n, k_heads, dim, dtype, 2), positions(n, 3)
+    for inverse in (False, True):
+        a, b = rotary.kv_rotary(q.to(DEV), p.to(DEV), k=k.to(DEV), inverse=inverse)
+        assert a.dtype == dtype and a.shape == q.shape and b.shape == k.shape
+        check(rotary, a, q, p, inverse)
+        check(rotary, b, k, p, inverse)
+    check(rotary, rotary.kv_rotary(k.to(DEV), p.to(DEV)), k, p)
+
+
+@pytest.mark.parametrize("scaling, more", [("linear", {}), ("base", {}), ("bands", {}), ("ramp", {}), ("ramp", dict(slow=2.0, fast=2.0)),
+                                           ("none", dict(magnitude=-0.5)), ("none", dict(frequencies=[100.0 - 3.7 * i for i in range(32)]))])
+def test_scalings_at_far_positions(scaling, more):
+    rotary = binding.Rotary(64, 64, base=500000.0, scaling=scaling, factor=1.0 if scaling == "none" else 16.0, original=4096, **more)
+    q = rows(300, 3, 64, torch.float32, 4)
+    p = positions(300, 5, FAR)
+    check(rotary, rotary.kv_rotary(q.to(DEV), p.to(DEV)), q, p)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+def test_parts_of_wider_rows_and_in_place(dtype):
+    n, hq, hk, dim = 37, 8, 2, 128
+    rotary = binding.Rotary(dim, 64)
+    for shift in (0, 1, 4):                                      # values that the rows are off a 16-byte address by
+        flat = rows(n, 1, (hq + 2 * hk) * dim + 24, dtype, 6).to(DEV).flatten()
+        wide = flat[shift:shift + n * ((hq + 2 * hk) * dim + 16)].view(n, -1)
+        parts = wide[:, :(hq + 2 * hk) * dim].unflatten(1, (hq + 2 * hk, dim))
+        q, k = parts[:, :hq], parts[:, hq:hq + hk]
+        p = positions(n, 7).to(DEV)
+        before, held_q, held_k = flat.clone(), q.cpu().clone(), k.cpu().clone()
+        a, b = rotary.kv_rotary(q, p, k=k)
+        assert torch.equal(flat, before)
+        check(rotary, a, held_q, p)
+        check(rotary, b, held_k, p)
+        c, d = rotary.kv_rotary(q, p, k=k, out=q, k_out=k)       # in place: the rest of the rows stays
+        assert c is q and d is k and torch.equal(q, a) and torch.equal(k, b)
+        now = flat.clone()
+        q.copy_(held_q), k.copy_(held_k)
+        assert torch.equal(flat, before) and not torch.equal(now, before)
+        # in place for one, elsewhere for the other
+        other = torch.full((n, hk * dim + 8), 7.0, dtype=dtype, device=DEV)
+        rotary.kv_rotary(q, p, k=k, out=q, k_out=other[:, :hk * dim].unflatten(1, (hk, dim)))
+        assert torch.equal(q, a) and torch.equal(other[:, :hk * dim].unflatten(1, (hk, dim)), b) and bool((other[:, hk * dim:] == 7.0).all())
+        q.copy_(held_q)
+
+
+def test_batched_rows_and_no_rows():
+    rotary = binding.Rotary(64)
+    q, p = rows(12, 3, 64, torch.bfloat16, 8), positions(12, 9)
+    flat = rotary.kv_rotary(q.to(DEV), p.to(DEV))
+    batched = rotary.kv_rotary(q.to(DEV).view(4, 3, 3, 64), p.to(DEV).view(4, 3))
+    assert batched.shape == (4, 3, 3, 64) and torch.equal(batched.view_as(flat), flat)
+    none = rotary.kv_rotary(q[:0].to(DEV), p[:0].to(DEV), k=q[:0].to(DEV))
+    assert none[0].shape == (0, 3, 64)
+    check(rotary, flat, q, p)
+
+
+def test_infinity_and_nan_stay_in_their_pair():
+    rotary = binding.Rotary(128)
+    q, p = rows(4, 2, 128, torch.float16, 10), positions(4, 11, 1000).clamp(min=1, max=1000)
+    clean = rotary.kv_rotary(q.to(DEV), p.to(DEV)).cpu()
+    q[1, 0, 5], q[2, 1, 69] = float("inf"), float("nan")
+    got = rotary.kv_rotary(q.to(DEV), p.to(DEV)).cpu()
+    bad = torch.zeros_like(q, dtype=torch.bool)
+    bad[1, 0, [5, 69]] = True
+    bad[2, 1, [5, 69]] = True
+    assert torch.equal(got[~bad], clean[~bad]) and not torch.isfinite(got[bad]).any()
+
+
+def test_inverse_is_the_gradient_and_takes_rows_back():
+    """<g, turn(x)> = <turn back(g), x> for every g: the transposed operation, also against differences of the formula."""
+    rotary = binding.Rotary(64, 48, scaling="ramp", factor=4.0)
+    x, g, p = rows(9, 2, 64, torch.float32, 12), rows(9, 2, 64, torch.float32, 13), positions(9, 14)
+    back = rotary.kv_rotary(g.to(DEV), p.to(DEV), inverse=True).cpu().double()
+    step = 2.0 ** -10
+    for i in (0, 5, 23, 24, 47, 48, 63):
+        d = torch.zeros_like(x, dtype=torch.float64)
+        d[..., i] = step
+        hi, _ = ref.turned(x.double() + d, p, rotary.frequencies, rotary.magnitude, False)
+        lo, _ = ref.turned(x.double() - d, p, rotary.frequencies, rotary.magnitude, False)
+        slope = ((hi - lo) / (2 * step) * g.double()).sum(-1)
+        # linear: differences are exact but for doubles' roundings; then the bound of the kernel's own arithmetic
+        _, bound = ref.turned(g, p, rotary.frequencies, rotary.magnitude, False, inverse=True)
+        near = ref.rounded(back, bound, torch.float32)[..., i] + 1e-9
+        assert bool(((back[..., i] - slope).abs() <= near).all())
+    plain = binding.Rotary(64, 48)
+    y = plain.kv_rotary(x.to(DEV), p.to(DEV))
+    again = plain.kv_rotary(y, p.to(DEV), inverse=True).cpu().double()
+    _, bound = ref.turned(x, p, plain.frequencies, 1.0, False)
+    # both turns' bounds; the second acts on values up to sqrt(2) of the first's
+    assert bool(((again - x.double()).abs() <= 4 * ref.rounded(x.double().abs() + 4, bound, torch.float32)).all())
+
+
+def test_offsets_beyond_32_bits():
+    heads, dim, n = 300, 512, 15000                              # 2.3e9 values
+    rotary = binding.Rotary(dim, 2)
+    x = torch.empty(n, heads, dim, dtype=torch.float16, device=DEV)
+    x.view(torch.int16).copy_((torch.arange(dim, device=DEV) * 37 % 15000).to(torch.int16))
+    p = positions(n, 15).to(DEV)
+    rotary.kv_rotary(x, p, out=x)
+    for at in (0, n // 2, n - 1):
+        base = (torch.arange(dim) * 37 % 15000).to(torch.int16).view(torch.float16).expand(1, heads, dim)
+        check(rotary, x[at:at + 1], base, p[at:at + 1].cpu())
+
+
+def test_captured_and_on_another_stream():
+    rotary = binding.Rotary(128)
+    q, k, p = rows(6, 4, 128, torch.bfloat16, 16).to(DEV), rows(6, 2, 128, torch.bfloat16, 17).to(DEV), positions(6, 18).to(DEV)
+    a, b = torch.empty_like(q), torch.empty_like(k)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for stream in (side, side.cuda_stream):
+        got = rotary.kv_rotary(q, p, k=k, stream=stream)
+        torch.cuda.synchronize()
+        check(rotary, got[0], q, p)
+    graph = torch.cuda.CUDAGraph()
+    rotary.kv_rotary(q, p, k=k, out=a, k_out=b)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        rotary.kv_rotary(q, p, k=k, out=a, k_out=b)
+    for step in range(4):
+        p += 1 + 1000 * step
+        q.mul_(-1)
+        a.zero_(), b.zero_()
+        graph.replay()
+        want = rotary.kv_rotary(q, p, k=k)
+        torch.cuda.synchronize()
+        assert torch.equal(a, want[0]) and torch.equal(b, want[1])
+        check(rotary, a, q, p)
