@@ -22,100 +22,317 @@ struct Fp4Weights {
     int64_t pitch;           // values of a (sequence, kv-head) in mass and past
 };
 
-// A wave takes a page of a kv-head past all columns.
+constexpr int WEIGHTS_HELD = 8;          // blocks of 16 columns that stay in LDS
+
+// What the rows of a block of 16 columns need beside q: register i of a lane's results is column 4i + g.
+struct Fp4RowSet {
+    float4 less[4];          // [g]: minus the logarithms, in powers of two
+    int4 hi[4];              // [g]: last tokens that the rows see
+    int first_hi, last_hi;   // of the rows that there are, least and largest
+    int pad[2];
+};
+
+// A lane's part of 16 columns' operand, and (lanes 0 .. 15) what their rows need; all lanes call.
 template <int HD, bool BF16>
-__global__ __launch_bounds__(256) void fp4_weights_kernel(Fp4Weights a, int page_groups) {
-    using P = Fp4Block<HD>;
-    constexpr int KW = HD / 32;
+__device__ inline void load_columns(const Fp4Weights &a, const Fp4Sequence &seq, int h, int column0, int columns, int lane,
+                                    uint4_t (&q)[HD / 32], float *less, int *hi) {
     const Fp4View &v = a.v;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c16 = lane & 15, g = lane >> 4;
-    const int group = int(blockIdx.x / uint32_t(v.H)), h = int(blockIdx.x - uint32_t(group) * v.H), b = blockIdx.y;
-    const Fp4Sequence seq(v, b);
-    for (int index = 4 * group + wave; int64_t(index) * FP4_PAGE < seq.held; index += 4 * page_groups) {
-        const int t0 = index * FP4_PAGE;
-        const int64_t page = seq.page(v, index);
-        // rows that may see a token of the page
-        const int first_row = max(int(min(int64_t(t0) - seq.pos0, int64_t(seq.n))), 0);
-        int end_row = seq.n;
-        if (a.window && t0 >= a.sinks) end_row = int(max(min(int64_t(t0) + FP4_PAGE - 1 + a.window - seq.pos0, int64_t(seq.n)), int64_t(0)));
-        float sum[4] = {0, 0, 0, 0};
-        if (page >= 0 && first_row < end_row) {
-            const uint8_t *block = v.pages + (page * v.H + h) * size_t(P::BYTES);
-            uint4_t k[4][KW];
+    const int c16 = lane & 15, g = lane >> 4;
+    const int column = column0 + 4 * (c16 & 3) + (c16 >> 2), of = column / v.G, head = h * v.G + column - of * v.G;
+    const int64_t row = seq.first + of;
+    const bool real = column < columns && row >= 0 && row < v.n_rows;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const int token = 16 * t + c16;
-                const uint32_t *from = reinterpret_cast<const uint32_t *>(block + P::K + token * (HD / 2) + g * (HD / 8));
-                const float scale = __uint_as_float(uint32_t(block[P::KS + token * (HD / FP4_GROUP) + g * (HD / 4) / FP4_GROUP]) << 23);
-#pragma unroll
-                for (int i = 0; i < KW; ++i) k[t][i] = row_operand<BF16>(from[i], scale);
-            }
-            const int64_t end_column = int64_t(end_row) * v.G;
-            for (int64_t column0 = int64_t(first_row) * v.G; column0 < end_column; column0 += 16) {
-                const auto place = [&](int64_t column, int64_t &row, int &head) {   // false: no such row of the call's tensors
-                    const int64_t of = column / v.G;
-                    row = seq.first + of, head = h * v.G + int(column - of * v.G);
-                    return column < end_column && row >= 0 && row < v.n_rows;
-                };
-                uint4_t q[KW];
-                int64_t row;
-                int head;
-                const bool real = place(column0 + 4 * (c16 & 3) + (c16 >> 2), row, head);
-#pragma unroll
-                for (int i = 0; i < KW; ++i) {
-                    q[i] = uint4_t{0, 0, 0, 0};
-                    if (real) q[i] = *reinterpret_cast<const uint4_t *>(a.q + row * a.q_stride + int64_t(head) * HD + g * (HD / 4) + 8 * i) ^ a.scale.sign;
-                }
-                a.scale.settle<BF16>(q);
-                float less[4];
-                int hi[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int64_t column = column0 + 4 * i + g;
-                    less[i] = -INFINITY, hi[i] = -1;
-                    if (place(column, row, head)) {
-                        const float lse = a.lse[row * (int64_t(v.H) * v.G) + head];
-                        if (lse != -INFINITY) less[i] = -(lse * FP4_LOG2E);   // (-infinity: a row that sees nothing)
-                        hi[i] = seq.pos0 + int(column / v.G);
-                    }
-                }
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    float4_t s = float4_t{0, 0, 0, 0};
-#pragma unroll
-                    for (int i = 0; i < KW; ++i) s = product16<BF16>(q[i], k[t][i], s);
-                    const int token = t0 + 16 * t + c16;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float p = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale.scale, less[i]));
-                        const bool seen = (token <= hi[i]) & (token < seq.held) & ((a.window == 0) | (token > hi[i] - a.window) | (token < a.sinks));
-                        sum[t] += seen ? p : 0.0f;
-                    }
-                }
-            }
-        }
-        float mine = 0.0f;
+    for (int i = 0; i < HD / 32; ++i) {
+        q[i] = uint4_t{0, 0, 0, 0};
+        if (real) q[i] = *reinterpret_cast<const uint4_t *>(a.q + row * a.q_stride + int64_t(head) * HD + g * (HD / 4) + 8 * i) ^ a.scale.sign;
+    }
+    *less = -INFINITY, *hi = max(seq.pos0 + min(of, seq.n - 1), -1);
+    if (real) {
+        const float lse = a.lse[row * (int64_t(v.H) * v.G) + head];
+        if (lse != -INFINITY) *less = -(lse * FP4_LOG2E);    // (-infinity: a row that sees nothing)
+    }
+    a.scale.settle<BF16>(q);
+}
+
+// The rows of a page on their way: of K a lane's quarter of four tokens' rows, and what one token had.
+template <int HD>
+struct Fp4KPage {
+    using P = Fp4Block<HD>;
+    static constexpr int KW = HD / 32;
+    uint32_t k[4][KW], ks[4];
+    float old;
+    __device__ inline void load(const uint8_t *block, const float *past, int c16, int g) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            const float all = column_sum(sum[t]);
-            if (g == t) mine = all;
+            const int token = 16 * t + c16;
+            const uint8_t *from = block + P::K + token * (HD / 2) + g * (HD / 8);
+            if constexpr (KW == 4) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(from);
+                k[t][0] = x.x, k[t][1] = x.y, k[t][2] = x.z, k[t][3] = x.w;
+            } else {
+                const uint2 x = *reinterpret_cast<const uint2 *>(from);
+                k[t][0] = x.x, k[t][1] = x.y;
+            }
+            ks[t] = block[P::KS + token * (HD / FP4_GROUP) + g * (HD / 4) / FP4_GROUP];
         }
-        const int token = t0 + lane;     // 16g + c16
-        if (token < seq.held && token < a.pitch) {
-            const int64_t at = (int64_t(b) * v.H + h) * a.pitch + token;
-            a.mass[at] = a.past && token < seq.pos0 ? a.past[at] + mine : mine;
+        old = *past;
+    }
+    template <bool BF16>
+    __device__ inline void operands(uint4_t (&to)[4][KW]) const {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < KW; ++i) to[t][i] = row_operand<BF16>(k[t][i], __uint_as_float(ks[t] << 23));
+    }
+};
+
+// Adds the weights that 16 columns give to the page's tokens.  NI: registers of a result that hold columns.
+template <int HD, bool BF16, int NI>
+__device__ inline void weigh_page(const Fp4Weights &a, const uint4_t (&q)[HD / 32], const float4 &less4, const int4 &hi4, bool masked,
+                                  const uint4_t (&k)[4][HD / 32], int t0, int end, int c16, float (&sum)[4]) {
+    const float less[4] = {less4.x, less4.y, less4.z, less4.w};
+    float4_t s[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) s[t] = float4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < HD / 32; ++i)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) s[t] = product16<BF16>(q[i], k[t][i], s[t]);
+    if (masked) {            // (wave-uniform)
+        const int hi[4] = {hi4.x, hi4.y, hi4.z, hi4.w};
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int token = t0 + 16 * t + c16;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const int lo = a.window ? hi[i] - a.window : -1;
+                const float p = __builtin_amdgcn_exp2f(fmaf(s[t][i], a.scale.scale, less[i]));
+                sum[t] += (token <= hi[i]) & (token < end) & ((token > lo) | (token < a.sinks)) ? p : 0.0f;
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        float p[NI];
+#pragma unroll
+        for (int i = 0; i < NI; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], a.scale.scale, less[i]));
+        if constexpr (NI == 4) sum[t] += (p[0] + p[1]) + (p[2] + p[3]);
+        else if constexpr (NI == 2) sum[t] += p[0] + p[1];
+        else sum[t] += p[0];
+    }
+}
+
+__device__ inline float token_sum(const float (&sum)[4], int g) {     // of token 16g + c16
+    float mine = 0.0f;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const float all = column_sum(sum[t]);
+        mine = g == t ? all : mine;
+    }
+    return mine;
+}
+
+// Which rows may see a token of the 64 from t0 on; every row of the sequence does see a token before `sinks` that it sees at all.
+struct Fp4RowsOf {
+    int first, end;
+    __device__ inline Fp4RowsOf(const Fp4Weights &a, const Fp4Sequence &seq, int t0) {
+        first = max(int(min(int64_t(t0) - seq.pos0, int64_t(seq.n))), 0);
+        end = seq.n;
+        if (a.window && t0 >= a.sinks) end = int(max(min(int64_t(t0) + FP4_PAGE - 1 + a.window - seq.pos0, int64_t(seq.n)), int64_t(0)));
+    }
+};
+
+// Few columns (up to 128): their operands stay, in LDS or, of one block, in registers, and pages stream past them, each wave's next one
+// on its way while one is weighed.  A workgroup takes 4 * pages_of_wave pages in a row, a wave every fourth.
+template <int HD, bool BF16, int NI, bool ONE>
+__global__ __launch_bounds__(256) void fp4_weights_kernel(Fp4Weights a, int pages_of_wave, int page_groups) {
+    using P = Fp4Block<HD>;
+    constexpr int KW = HD / 32, HELD = ONE ? 1 : WEIGHTS_HELD;
+    __shared__ uint4_t held[HELD][KW][64];
+    __shared__ Fp4RowSet sets[HELD];
+    const Fp4View &v = a.v;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c16 = lane & 15, g = lane >> 4;
+    const int h = blockIdx.x % uint32_t(v.H), b = blockIdx.y;
+    int group = int(blockIdx.x / uint32_t(v.H));
+    const Fp4Sequence seq(v, b);
+    const int columns = seq.n * v.G, blocks = (columns + 15) / 16;
+    const int table_end = (seq.held + FP4_PAGE - 1) / FP4_PAGE;
+    if (4 * pages_of_wave * group >= table_end) return;
+    uint4_t q[KW];
+    for (int n = wave; n < (ONE ? 4 : blocks); n += 4) {
+        float less;
+        int hi;
+        const int block = ONE ? 0 : n;
+        load_columns<HD, BF16>(a, seq, h, 16 * block, columns, lane, q, &less, &hi);
+        if (!ONE || wave == 0) {
+            if (!ONE) {
+#pragma unroll
+                for (int i = 0; i < KW; ++i) held[block][i][lane] = q[i];
+            }
+            Fp4RowSet &set = sets[block];
+            if (lane < 16) reinterpret_cast<float *>(set.less)[lane] = less, reinterpret_cast<int *>(set.hi)[lane] = hi;   // (lane 4g + i: column 4i + g)
+            if (lane == 0) set.first_hi = hi;
+            if (lane == 15) set.last_hi = hi;
+        }
+    }
+    __syncthreads();
+    const float *past = a.past ? a.past + (int64_t(b) * v.H + h) * a.pitch : nullptr;
+    float *mass = a.mass + (int64_t(b) * v.H + h) * a.pitch;
+    const int past_end = int(min(int64_t(min(seq.held, seq.pos0)), a.pitch)), mass_end = int(min(int64_t(seq.held), a.pitch));
+    for (; 4 * pages_of_wave * group < table_end; group += page_groups) {
+        // the wave's pages, one to a lane
+        const int mine = 4 * (pages_of_wave * group + lane) + wave;
+        const bool there = lane < pages_of_wave && mine < table_end;
+        int page = -1;
+        if (there) {
+            const Fp4RowsOf rows(a, seq, mine * FP4_PAGE);
+            if (rows.first < rows.end) page = int(seq.page(v, mine));
+        }
+        uint64_t todo = __ballot(page >= 0), idle = __ballot(there && page < 0);
+        while (idle) {       // nothing sees these
+            const int j = __builtin_ctzll(idle), token = (4 * (pages_of_wave * group + j) + wave) * FP4_PAGE + lane;
+            idle &= idle - 1;
+            if (token < mass_end) mass[token] = past && token < past_end ? past[token] : 0.0f;
+        }
+        if (!todo) continue;
+        Fp4KPage<HD> in[2];
+        int at[2];           // pages of the sequence
+        const auto fetch = [&](int to, int j) {
+            at[to] = 4 * (pages_of_wave * group + j) + wave;
+            const int token = at[to] * FP4_PAGE + lane;
+            const float *old = past && token < past_end ? past + token : reinterpret_cast<const float *>(v.pages);
+            in[to].load(v.pages + (int64_t(__builtin_amdgcn_readlane(page, j)) * v.H + h) * size_t(P::BYTES), old, c16, g);
+        };
+        const auto compute = [&](int which) {
+            uint4_t k[4][KW];
+            in[which].template operands<BF16>(k);
+            const int t0 = at[which] * FP4_PAGE;
+            float sum[4] = {0, 0, 0, 0};
+            for (int n = 0; n < (ONE ? 1 : blocks); ++n) {
+                const Fp4RowSet &set = sets[n];
+                const int first_hi = __builtin_amdgcn_readfirstlane(set.first_hi), last_hi = __builtin_amdgcn_readfirstlane(set.last_hi);
+                const bool masked = t0 + FP4_PAGE > min(seq.held, first_hi + 1) || (a.window && t0 <= last_hi - a.window);
+                if (!ONE) {
+#pragma unroll
+                    for (int i = 0; i < KW; ++i) q[i] = held[n][i][lane];
+                }
+                weigh_page<HD, BF16, NI>(a, q, set.less[g], set.hi[g], masked, k, t0, seq.held, c16, sum);
+            }
+            const int token = t0 + lane;
+            const float all = token_sum(sum, g);
+            if (token < mass_end) mass[token] = past && token < past_end ? in[which].old + all : all;
+        };
+        // every fetch is made, behind the last page that one again
+        const auto next = [&]() {
+            const int j = __builtin_ctzll(todo);
+            if (todo & (todo - 1)) todo &= todo - 1;
+            return j;
+        };
+        int left = __popcll(todo);
+        fetch(0, next());
+        while (true) {
+            fetch(1, next());
+            compute(0);
+            if (--left == 0) break;
+            fetch(0, next());
+            compute(1);
+            if (--left == 0) break;
         }
     }
 }
+
+// Many columns: a wave keeps the operands of a page, the columns pass through LDS, 64 at a time, in two buffers in turn.
+template <int HD, bool BF16>
+__global__ __launch_bounds__(256) void fp4_weights_tile_kernel(Fp4Weights a, int page_groups) {
+    using P = Fp4Block<HD>;
+    constexpr int KW = HD / 32;
+    __shared__ uint4_t staged[2][4][KW][64];
+    __shared__ Fp4RowSet sets[2][4];
+    const Fp4View &v = a.v;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c16 = lane & 15, g = lane >> 4;
+    const int h = blockIdx.x % uint32_t(v.H), b = blockIdx.y;
+    const Fp4Sequence seq(v, b);
+    const int columns = seq.n * v.G, table_end = (seq.held + FP4_PAGE - 1) / FP4_PAGE;
+    const float *past = a.past ? a.past + (int64_t(b) * v.H + h) * a.pitch : nullptr;
+    float *mass = a.mass + (int64_t(b) * v.H + h) * a.pitch;
+    const int past_end = int(min(int64_t(min(seq.held, seq.pos0)), a.pitch)), mass_end = int(min(int64_t(seq.held), a.pitch));
+    for (int group = int(blockIdx.x / uint32_t(v.H)); 4 * group < table_end; group += page_groups) {
+        const int index = 4 * group + wave, t0 = index * FP4_PAGE, token = t0 + lane;
+        const Fp4RowsOf lowest(a, seq, 4 * group * FP4_PAGE), highest(a, seq, (4 * group + 3) * FP4_PAGE);
+        const int row0 = lowest.first, row_end = max(lowest.end, highest.end);
+        const int column0 = row0 * v.G / 64 * 64, column_end = row_end * v.G;
+        const int64_t page = index < table_end ? seq.page(v, index) : -1;
+        Fp4KPage<HD> in;
+        in.load(v.pages + (max(page, int64_t(0)) * v.H + h) * size_t(P::BYTES),
+                past && token < past_end ? past + token : reinterpret_cast<const float *>(v.pages), c16, g);
+        uint4_t k[4][KW];
+        in.template operands<BF16>(k);
+        float sum[4] = {0, 0, 0, 0};
+        uint4_t q[KW];
+        float less;
+        int hi;
+        const auto store = [&](int to) {
+#pragma unroll
+            for (int i = 0; i < KW; ++i) staged[to][wave][i][lane] = q[i];
+            Fp4RowSet &set = sets[to][wave];
+            if (lane < 16) reinterpret_cast<float *>(set.less)[lane] = less, reinterpret_cast<int *>(set.hi)[lane] = hi;
+            if (lane == 0) set.first_hi = hi;
+            if (lane == 15) set.last_hi = hi;
+        };
+        if (column0 < column_end) {
+            load_columns<HD, BF16>(a, seq, h, column0 + 16 * wave, columns, lane, q, &less, &hi);
+            store(0);
+        }
+        __syncthreads();
+        int now = 0;
+        for (int column = column0; column < column_end; column += 64, now ^= 1) {
+            const bool more = column + 64 < column_end;
+            if (more) load_columns<HD, BF16>(a, seq, h, column + 64 + 16 * wave, columns, lane, q, &less, &hi);
+            if (page >= 0) {
+                float part[4] = {0, 0, 0, 0};
+                for (int n = 0; n < 4; ++n) {
+                    const Fp4RowSet &set = sets[now][n];
+                    const int first_hi = __builtin_amdgcn_readfirstlane(set.first_hi), last_hi = __builtin_amdgcn_readfirstlane(set.last_hi);
+                    if (last_hi < t0 || (a.window && t0 >= a.sinks && t0 + FP4_PAGE - 1 <= first_hi - a.window)) continue;
+                    const bool masked = t0 + FP4_PAGE > min(seq.held, first_hi + 1) || (a.window && t0 <= last_hi - a.window);
+                    uint4_t p[KW];
+#pragma unroll
+                    for (int i = 0; i < KW; ++i) p[i] = staged[now][n][i][lane];
+                    weigh_page<HD, BF16, 4>(a, p, set.less[g], set.hi[g], masked, k, t0, seq.held, c16, part);
+                }
+#pragma unroll
+                for (int t = 0; t < 4; ++t) sum[t] += part[t];
+            }
+            if (more) store(now ^ 1);
+            __syncthreads();
+        }
+        const float all = token_sum(sum, g);
+        if (token < mass_end) mass[token] = past && token < past_end ? in.old + all : all;
+    }
+}
+
+// Waves that a call is spread over before a wave takes several pages.
+constexpr int64_t WEIGHTS_WAVES = 8192;
 
 int launch_fp4_weights(const kv_fp4_cache *c, const Fp4View &v, const void *q, int64_t q_stride, bool bf16, float sm_scale, int window,
                        int sinks, const float *lse, const float *past, float *mass, int64_t mass_tokens, hipStream_t s) {
     const Fp4Weights a{v, static_cast<const uint16_t *>(q), q_stride, lse, Fp4Scale::of(sm_scale * FP4_LOG2E), window, sinks,
                        past, mass, mass_tokens};
-    const int64_t pages = std::min<int64_t>((v.batch.table_pages + 3) / 4, 4096);
-    if (pages * v.H > FP4_GROUPS_MOST) return KV_ERR_UNSUPPORTED;
-    const dim3 grid = dim3(uint32_t(pages * v.H), uint32_t(v.batch.batch));
-#define LAUNCH(HD, BF) hipLaunchKernelGGL((fp4_weights_kernel<HD, BF>), grid, dim3(256), 0, s, a, int(pages))
+    const int64_t columns = int64_t(v.batch.max_new) * v.G, most = int64_t(v.batch.table_pages) * v.H * v.batch.batch;   // pages
+    const bool tiles = columns > 16 * WEIGHTS_HELD;
+    const int each = tiles ? 1 : int(std::min<int64_t>(std::max<int64_t>(most / WEIGHTS_WAVES, 1), 16));
+    const int64_t groups = std::min<int64_t>((v.batch.table_pages + 4 * each - 1) / (4 * each), 4096);
+    if (groups * v.H > FP4_GROUPS_MOST) return KV_ERR_UNSUPPORTED;
+    const dim3 grid = dim3(uint32_t(groups * v.H), uint32_t(v.batch.batch));
+#define LAUNCH(HD, BF)                                                                                                              \
+    do {                                                                                                                            \
+        if (tiles) hipLaunchKernelGGL((fp4_weights_tile_kernel<HD, BF>), grid, dim3(256), 0, s, a, int(groups));                    \
+        else if (columns > 16) hipLaunchKernelGGL((fp4_weights_kernel<HD, BF, 4, false>), grid, dim3(256), 0, s, a, each, int(groups)); \
+        else if (columns > 8) hipLaunchKernelGGL((fp4_weights_kernel<HD, BF, 4, true>), grid, dim3(256), 0, s, a, each, int(groups));   \
+        else if (columns > 4) hipLaunchKernelGGL((fp4_weights_kernel<HD, BF, 2, true>), grid, dim3(256), 0, s, a, each, int(groups));   \
+        else hipLaunchKernelGGL((fp4_weights_kernel<HD, BF, 1, true>), grid, dim3(256), 0, s, a, each, int(groups));                \
+    } while (0)
     if (c->cfg.head_dim == 128) {
         if (bf16) LAUNCH(128, true); else LAUNCH(128, false);
     } else {
