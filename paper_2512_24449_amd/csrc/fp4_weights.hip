@@ -32,27 +32,45 @@ struct Fp4RowSet {
     int pad[2];
 };
 
-// A lane's part of 16 columns' operand, and (lanes 0 .. 15) what their rows need; all lanes call.
+// A lane's part of 16 columns' operand on its way, and (lanes 0 .. 15) of what their rows need.
 template <int HD, bool BF16>
-__device__ inline void load_columns(const Fp4Weights &a, const Fp4Sequence &seq, int h, int column0, int columns, int lane,
-                                    uint4_t (&q)[HD / 32], float *less, int *hi) {
-    const Fp4View &v = a.v;
-    const int c16 = lane & 15, g = lane >> 4;
-    const int column = column0 + 4 * (c16 & 3) + (c16 >> 2), of = column / v.G, head = h * v.G + column - of * v.G;
-    const int64_t row = seq.first + of;
-    const bool real = column < columns && row >= 0 && row < v.n_rows;
+struct Fp4Columns {
+    static constexpr int KW = HD / 32;
+    uint4_t q[KW];
+    float lse;
+    int hi;
+    bool real;
+    // Every lane loads, from somewhere: loads that are made on some paths only would be waited for one by one.
+    __device__ inline void load(const Fp4Weights &a, const Fp4Sequence &seq, int h, int column0, int columns, int lane) {
+        const Fp4View &v = a.v;
+        const int c16 = lane & 15, g = lane >> 4;
+        const int column = column0 + 4 * (c16 & 3) + (c16 >> 2), of = column / v.G, head = h * v.G + column - of * v.G;
+        const int64_t row = seq.first + of;
+        real = column < columns && row >= 0 && row < v.n_rows;
+        const uint16_t *from = a.q + row * a.q_stride + int64_t(head) * HD + g * (HD / 4);
+        const float *sum = a.lse + (row * (int64_t(v.H) * v.G) + head);
+        from = real ? from : reinterpret_cast<const uint16_t *>(v.pages);
+        sum = real ? sum : reinterpret_cast<const float *>(v.pages);
 #pragma unroll
-    for (int i = 0; i < HD / 32; ++i) {
-        q[i] = uint4_t{0, 0, 0, 0};
-        if (real) q[i] = *reinterpret_cast<const uint4_t *>(a.q + row * a.q_stride + int64_t(head) * HD + g * (HD / 4) + 8 * i) ^ a.scale.sign;
+        for (int i = 0; i < KW; ++i) q[i] = *reinterpret_cast<const uint4_t *>(from + 8 * i);
+        lse = *sum;
+        hi = max(seq.pos0 + min(of, seq.n - 1), -1);
     }
-    *less = -INFINITY, *hi = max(seq.pos0 + min(of, seq.n - 1), -1);
-    if (real) {
-        const float lse = a.lse[row * (int64_t(v.H) * v.G) + head];
-        if (lse != -INFINITY) *less = -(lse * FP4_LOG2E);    // (-infinity: a row that sees nothing)
+    __device__ inline void settle(const Fp4Weights &a) {
+#pragma unroll
+        for (int i = 0; i < KW; ++i) q[i] = real ? q[i] ^ a.scale.sign : uint4_t{0, 0, 0, 0};
+        a.scale.settle<BF16>(q);
     }
-    a.scale.settle<BF16>(q);
-}
+    __device__ inline void store(Fp4RowSet &set, int lane) const {
+        // (-infinity: a row that sees nothing)
+        if (lane < 16) {
+            reinterpret_cast<float *>(set.less)[lane] = real && lse != -INFINITY ? -(lse * FP4_LOG2E) : -INFINITY;
+            reinterpret_cast<int *>(set.hi)[lane] = hi;      // (lane 4g + i: column 4i + g)
+        }
+        if (lane == 0) set.first_hi = hi;
+        if (lane == 15) set.last_hi = hi;
+    }
+};
 
 // The rows of a page on their way: of K a lane's quarter of four tokens' rows, and what one token had.
 template <int HD>
@@ -86,32 +104,20 @@ struct Fp4KPage {
     }
 };
 
-// Adds the weights that 16 columns give to the page's tokens.  NI: registers of a result that hold columns.
-template <int HD, bool BF16, int NI>
-__device__ inline void weigh_page(const Fp4Weights &a, const uint4_t (&q)[HD / 32], const float4 &less4, const int4 &hi4, bool masked,
-                                  const uint4_t (&k)[4][HD / 32], int t0, int end, int c16, float (&sum)[4]) {
-    const float less[4] = {less4.x, less4.y, less4.z, less4.w};
-    float4_t s[4];
+template <int HD, bool BF16>
+__device__ inline void scores(const uint4_t (&q)[HD / 32], const uint4_t (&k)[4][HD / 32], float4_t (&s)[4]) {
 #pragma unroll
     for (int t = 0; t < 4; ++t) s[t] = float4_t{0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < HD / 32; ++i)
 #pragma unroll
         for (int t = 0; t < 4; ++t) s[t] = product16<BF16>(q[i], k[t][i], s[t]);
-    if (masked) {            // (wave-uniform)
-        const int hi[4] = {hi4.x, hi4.y, hi4.z, hi4.w};
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int token = t0 + 16 * t + c16;
-#pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const int lo = a.window ? hi[i] - a.window : -1;
-                const float p = __builtin_amdgcn_exp2f(fmaf(s[t][i], a.scale.scale, less[i]));
-                sum[t] += (token <= hi[i]) & (token < end) & ((token > lo) | (token < a.sinks)) ? p : 0.0f;
-            }
-        }
-        return;
-    }
+}
+
+// Adds the weights that 16 columns give to the page's tokens, all of which they see.  NI: registers of a result that hold columns.
+template <int NI>
+__device__ inline void weigh_whole(const Fp4Weights &a, const float4_t (&s)[4], const float4 &less4, float (&sum)[4]) {
+    const float less[4] = {less4.x, less4.y, less4.z, less4.w};
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
         float p[NI];
@@ -121,6 +127,29 @@ __device__ inline void weigh_page(const Fp4Weights &a, const uint4_t (&q)[HD / 3
         else if constexpr (NI == 2) sum[t] += p[0] + p[1];
         else sum[t] += p[0];
     }
+}
+
+// The same where some do not see some.
+template <int NI>
+__device__ inline void weigh_some(const Fp4Weights &a, const float4_t (&s)[4], const float4 &less4, const int4 &hi4, int t0, int end, int c16,
+                                  float (&sum)[4]) {
+    const float less[4] = {less4.x, less4.y, less4.z, less4.w};
+    const int hi[4] = {hi4.x, hi4.y, hi4.z, hi4.w};
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const int token = t0 + 16 * t + c16;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int lo = a.window ? hi[i] - a.window : -1;
+            const float p = __builtin_amdgcn_exp2f(fmaf(s[t][i], a.scale.scale, less[i]));
+            sum[t] += (token <= hi[i]) & (token < end) & ((token > lo) | (token < a.sinks)) ? p : 0.0f;
+        }
+    }
+}
+
+// Whether rows that see up to first_hi .. last_hi see all tokens of the page at t0.
+__device__ inline bool sees_whole(const Fp4Weights &a, int t0, int end, int first_hi, int last_hi) {
+    return t0 + FP4_PAGE <= min(end, first_hi + 1) && !(a.window && t0 <= last_hi - a.window);
 }
 
 __device__ inline float token_sum(const float (&sum)[4], int g) {     // of token 16g + c16
@@ -159,22 +188,16 @@ __global__ __launch_bounds__(256) void fp4_weights_kernel(Fp4Weights a, int page
     const int columns = seq.n * v.G, blocks = (columns + 15) / 16;
     const int table_end = (seq.held + FP4_PAGE - 1) / FP4_PAGE;
     if (4 * pages_of_wave * group >= table_end) return;
-    uint4_t q[KW];
+    Fp4Columns<HD, BF16> cols;
     for (int n = wave; n < (ONE ? 4 : blocks); n += 4) {
-        float less;
-        int hi;
         const int block = ONE ? 0 : n;
-        load_columns<HD, BF16>(a, seq, h, 16 * block, columns, lane, q, &less, &hi);
-        if (!ONE || wave == 0) {
-            if (!ONE) {
+        cols.load(a, seq, h, 16 * block, columns, lane);
+        cols.settle(a);
+        if (!ONE) {
 #pragma unroll
-                for (int i = 0; i < KW; ++i) held[block][i][lane] = q[i];
-            }
-            Fp4RowSet &set = sets[block];
-            if (lane < 16) reinterpret_cast<float *>(set.less)[lane] = less, reinterpret_cast<int *>(set.hi)[lane] = hi;   // (lane 4g + i: column 4i + g)
-            if (lane == 0) set.first_hi = hi;
-            if (lane == 15) set.last_hi = hi;
+            for (int i = 0; i < KW; ++i) held[block][i][lane] = cols.q[i];
         }
+        if (!ONE || wave == 0) cols.store(sets[block], lane);
     }
     __syncthreads();
     const float *past = a.past ? a.past + (int64_t(b) * v.H + h) * a.pitch : nullptr;
@@ -209,15 +232,19 @@ __global__ __launch_bounds__(256) void fp4_weights_kernel(Fp4Weights a, int page
             in[which].template operands<BF16>(k);
             const int t0 = at[which] * FP4_PAGE;
             float sum[4] = {0, 0, 0, 0};
+            float4_t s[4];
+            const bool whole = sees_whole(a, t0, seq.held, max(seq.pos0, -1), max(seq.pos0 + seq.n - 1, -1));   // (wave-uniform)
             for (int n = 0; n < (ONE ? 1 : blocks); ++n) {
-                const Fp4RowSet &set = sets[n];
-                const int first_hi = __builtin_amdgcn_readfirstlane(set.first_hi), last_hi = __builtin_amdgcn_readfirstlane(set.last_hi);
-                const bool masked = t0 + FP4_PAGE > min(seq.held, first_hi + 1) || (a.window && t0 <= last_hi - a.window);
-                if (!ONE) {
+                if constexpr (ONE) {
+                    scores<HD, BF16>(cols.q, k, s);
+                } else {
+                    uint4_t q[KW];
 #pragma unroll
                     for (int i = 0; i < KW; ++i) q[i] = held[n][i][lane];
+                    scores<HD, BF16>(q, k, s);
                 }
-                weigh_page<HD, BF16, NI>(a, q, set.less[g], set.hi[g], masked, k, t0, seq.held, c16, sum);
+                if (whole) weigh_whole<NI>(a, s, sets[n].less[g], sum);
+                else weigh_some<NI>(a, s, sets[n].less[g], sets[n].hi[g], t0, seq.held, c16, sum);
             }
             const int token = t0 + lane;
             const float all = token_sum(sum, g);
@@ -269,42 +296,54 @@ __global__ __launch_bounds__(256) void fp4_weights_tile_kernel(Fp4Weights a, int
         uint4_t k[4][KW];
         in.template operands<BF16>(k);
         float sum[4] = {0, 0, 0, 0};
-        uint4_t q[KW];
-        float less;
-        int hi;
+        Fp4Columns<HD, BF16> cols;
         const auto store = [&](int to) {
+            cols.settle(a);
 #pragma unroll
-            for (int i = 0; i < KW; ++i) staged[to][wave][i][lane] = q[i];
-            Fp4RowSet &set = sets[to][wave];
-            if (lane < 16) reinterpret_cast<float *>(set.less)[lane] = less, reinterpret_cast<int *>(set.hi)[lane] = hi;
-            if (lane == 0) set.first_hi = hi;
-            if (lane == 15) set.last_hi = hi;
+            for (int i = 0; i < KW; ++i) staged[to][wave][i][lane] = cols.q[i];
+            cols.store(sets[to][wave], lane);
         };
         if (column0 < column_end) {
-            load_columns<HD, BF16>(a, seq, h, column0 + 16 * wave, columns, lane, q, &less, &hi);
+            cols.load(a, seq, h, column0 + 16 * wave, columns, lane);
             store(0);
         }
         __syncthreads();
         int now = 0;
         for (int column = column0; column < column_end; column += 64, now ^= 1) {
-            const bool more = column + 64 < column_end;
-            if (more) load_columns<HD, BF16>(a, seq, h, column + 64 + 16 * wave, columns, lane, q, &less, &hi);
-            if (page >= 0) {
-                float part[4] = {0, 0, 0, 0};
+            // (behind the last ones those again, which nobody reads)
+            cols.load(a, seq, h, min(column + 64, (column_end - 1) / 64 * 64) + 16 * wave, columns, lane);
+            const int first_hi = __builtin_amdgcn_readfirstlane(sets[now][0].first_hi), last_hi = __builtin_amdgcn_readfirstlane(sets[now][3].last_hi);
+            float part[4] = {0, 0, 0, 0};
+            const uint4_t(*tile)[KW][64] = staged[now];
+            if (page < 0 || last_hi < t0 || (a.window && t0 >= a.sinks && t0 + FP4_PAGE - 1 <= first_hi - a.window)) {
+            } else if (sees_whole(a, t0, seq.held, first_hi, last_hi)) {
+                uint4_t q[2][KW];
+                float4_t s[2][4];
+#pragma unroll
+                for (int i = 0; i < KW; ++i) q[0][i] = tile[0][i][lane];
+#pragma unroll
                 for (int n = 0; n < 4; ++n) {
-                    const Fp4RowSet &set = sets[now][n];
-                    const int first_hi = __builtin_amdgcn_readfirstlane(set.first_hi), last_hi = __builtin_amdgcn_readfirstlane(set.last_hi);
-                    if (last_hi < t0 || (a.window && t0 >= a.sinks && t0 + FP4_PAGE - 1 <= first_hi - a.window)) continue;
-                    const bool masked = t0 + FP4_PAGE > min(seq.held, first_hi + 1) || (a.window && t0 <= last_hi - a.window);
-                    uint4_t p[KW];
+                    if (n < 3) {
 #pragma unroll
-                    for (int i = 0; i < KW; ++i) p[i] = staged[now][n][i][lane];
-                    weigh_page<HD, BF16, 4>(a, p, set.less[g], set.hi[g], masked, k, t0, seq.held, c16, part);
+                        for (int i = 0; i < KW; ++i) q[(n + 1) & 1][i] = tile[n + 1][i][lane];
+                    }
+                    scores<HD, BF16>(q[n & 1], k, s[n & 1]);
+                    if (n > 0) weigh_whole<4>(a, s[(n - 1) & 1], sets[now][n - 1].less[g], part);
                 }
+                weigh_whole<4>(a, s[1], sets[now][3].less[g], part);
+            } else {
+                for (int n = 0; n < 4; ++n) {
+                    uint4_t q[KW];
+                    float4_t s[4];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) sum[t] += part[t];
+                    for (int i = 0; i < KW; ++i) q[i] = tile[n][i][lane];
+                    scores<HD, BF16>(q, k, s);
+                    weigh_some<4>(a, s, sets[now][n].less[g], sets[now][n].hi[g], t0, seq.held, c16, part);
+                }
             }
-            if (more) store(now ^ 1);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) sum[t] += part[t];
+            store(now ^ 1);
             __syncthreads();
         }
         const float all = token_sum(sum, g);
