@@ -15,11 +15,13 @@ struct Fp4Weights {
     const uint16_t *q;
     int64_t q_stride;
     const float *lse;
-    Fp4Scale scale;
+    float scale;             // for powers of two
     int window, sinks;
     const float *past;
     float *mass;
     int64_t pitch;           // values of a (sequence, kv-head) in mass and past
+    float *part;             // not null: sums of each split of the columns, [splits][batch][H][table_pages * 64]
+    int splits;
 };
 
 constexpr int WEIGHTS_HELD = 8;          // blocks of 16 columns that stay in LDS
@@ -32,36 +34,46 @@ struct Fp4RowSet {
     int pad[2];
 };
 
-// A lane's part of 16 columns' operand on its way, and (lanes 0 .. 15) of what their rows need.
+// A lane's part of 16 columns' operand on its way, and (lanes 0 .. 15) of what their rows need; then 64 columns further on.
+// An infinity in q needs no care: the row's lse is NaN then.
 template <int HD, bool BF16>
 struct Fp4Columns {
     static constexpr int KW = HD / 32;
     uint4_t q[KW];
     float lse;
-    int hi;
+    int of, beside;          // row and head of the column
+    int row;                 // of what was loaded
     bool real;
+    __device__ inline void start(const Fp4Weights &a, int column0, int lane) {
+        const int column = column0 + 4 * (lane & 3) + ((lane & 15) >> 2);
+        of = column / a.v.G, beside = column - of * a.v.G;
+    }
     // Every lane loads, from somewhere: loads that are made on some paths only would be waited for one by one.
-    __device__ inline void load(const Fp4Weights &a, const Fp4Sequence &seq, int h, int column0, int columns, int lane) {
+    __device__ inline void load(const Fp4Weights &a, const Fp4Sequence &seq, int h, int lane) {
         const Fp4View &v = a.v;
-        const int c16 = lane & 15, g = lane >> 4;
-        const int column = column0 + 4 * (c16 & 3) + (c16 >> 2), of = column / v.G, head = h * v.G + column - of * v.G;
-        const int64_t row = seq.first + of;
-        real = column < columns && row >= 0 && row < v.n_rows;
-        const uint16_t *from = a.q + row * a.q_stride + int64_t(head) * HD + g * (HD / 4);
-        const float *sum = a.lse + (row * (int64_t(v.H) * v.G) + head);
+        const int64_t at = seq.first + of;
+        const int head = h * v.G + beside;
+        real = of < seq.n && at >= 0 && at < v.n_rows;
+        const uint16_t *from = a.q + at * a.q_stride + int64_t(head) * HD + (lane >> 4) * (HD / 4);
+        const float *sum = a.lse + (at * (int64_t(v.H) * v.G) + head);
         from = real ? from : reinterpret_cast<const uint16_t *>(v.pages);
         sum = real ? sum : reinterpret_cast<const float *>(v.pages);
 #pragma unroll
         for (int i = 0; i < KW; ++i) q[i] = *reinterpret_cast<const uint4_t *>(from + 8 * i);
         lse = *sum;
-        hi = max(seq.pos0 + min(of, seq.n - 1), -1);
+        row = of;
+    }
+    __device__ inline void advance(int G, int rows64, int heads64) {     // 64 / G, 64 % G
+        of += rows64, beside += heads64;
+        if (beside >= G) beside -= G, ++of;
     }
     __device__ inline void settle(const Fp4Weights &a) {
+        if (__all(real) && a.scale != 0.0f) return;
 #pragma unroll
-        for (int i = 0; i < KW; ++i) q[i] = real ? q[i] ^ a.scale.sign : uint4_t{0, 0, 0, 0};
-        a.scale.settle<BF16>(q);
+        for (int i = 0; i < KW; ++i) q[i] = real && a.scale != 0.0f ? q[i] : uint4_t{0, 0, 0, 0};
     }
-    __device__ inline void store(Fp4RowSet &set, int lane) const {
+    __device__ inline void store(Fp4RowSet &set, const Fp4Sequence &seq, int lane) const {
+        const int hi = max(seq.pos0 + min(row, seq.n - 1), -1);
         // (-infinity: a row that sees nothing)
         if (lane < 16) {
             reinterpret_cast<float *>(set.less)[lane] = real && lse != -INFINITY ? -(lse * FP4_LOG2E) : -INFINITY;
@@ -72,14 +84,13 @@ struct Fp4Columns {
     }
 };
 
-// The rows of a page on their way: of K a lane's quarter of four tokens' rows, and what one token had.
+// The rows of a page on their way: of K a lane's quarter of four tokens' rows.
 template <int HD>
 struct Fp4KPage {
     using P = Fp4Block<HD>;
     static constexpr int KW = HD / 32;
     uint32_t k[4][KW], ks[4];
-    float old;
-    __device__ inline void load(const uint8_t *block, const float *past, int c16, int g) {
+    __device__ inline void load(const uint8_t *block, int c16, int g) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             const int token = 16 * t + c16;
@@ -93,7 +104,6 @@ struct Fp4KPage {
             }
             ks[t] = block[P::KS + token * (HD / FP4_GROUP) + g * (HD / 4) / FP4_GROUP];
         }
-        old = *past;
     }
     template <bool BF16>
     __device__ inline void operands(uint4_t (&to)[4][KW]) const {
@@ -122,7 +132,7 @@ __device__ inline void weigh_whole(const Fp4Weights &a, const float4_t (&s)[4], 
     for (int t = 0; t < 4; ++t) {
         float p[NI];
 #pragma unroll
-        for (int i = 0; i < NI; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], a.scale.scale, less[i]));
+        for (int i = 0; i < NI; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], a.scale, less[i]));
         if constexpr (NI == 4) sum[t] += (p[0] + p[1]) + (p[2] + p[3]);
         else if constexpr (NI == 2) sum[t] += p[0] + p[1];
         else sum[t] += p[0];
@@ -141,7 +151,7 @@ __device__ inline void weigh_some(const Fp4Weights &a, const float4_t (&s)[4], c
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
             const int lo = a.window ? hi[i] - a.window : -1;
-            const float p = __builtin_amdgcn_exp2f(fmaf(s[t][i], a.scale.scale, less[i]));
+            const float p = __builtin_amdgcn_exp2f(fmaf(s[t][i], a.scale, less[i]));
             sum[t] += (token <= hi[i]) & (token < end) & ((token > lo) | (token < a.sinks)) ? p : 0.0f;
         }
     }
@@ -191,13 +201,14 @@ __global__ __launch_bounds__(256) void fp4_weights_kernel(Fp4Weights a, int page
     Fp4Columns<HD, BF16> cols;
     for (int n = wave; n < (ONE ? 4 : blocks); n += 4) {
         const int block = ONE ? 0 : n;
-        cols.load(a, seq, h, 16 * block, columns, lane);
+        cols.start(a, 16 * block, lane);
+        cols.load(a, seq, h, lane);
         cols.settle(a);
         if (!ONE) {
 #pragma unroll
             for (int i = 0; i < KW; ++i) held[block][i][lane] = cols.q[i];
         }
-        if (!ONE || wave == 0) cols.store(sets[block], lane);
+        if (!ONE || wave == 0) cols.store(sets[block], seq, lane);
     }
     __syncthreads();
     const float *past = a.past ? a.past + (int64_t(b) * v.H + h) * a.pitch : nullptr;
@@ -221,11 +232,12 @@ __global__ __launch_bounds__(256) void fp4_weights_kernel(Fp4Weights a, int page
         if (!todo) continue;
         Fp4KPage<HD> in[2];
         int at[2];           // pages of the sequence
+        float old[2];        // what the lane's token had
         const auto fetch = [&](int to, int j) {
             at[to] = 4 * (pages_of_wave * group + j) + wave;
             const int token = at[to] * FP4_PAGE + lane;
-            const float *old = past && token < past_end ? past + token : reinterpret_cast<const float *>(v.pages);
-            in[to].load(v.pages + (int64_t(__builtin_amdgcn_readlane(page, j)) * v.H + h) * size_t(P::BYTES), old, c16, g);
+            in[to].load(v.pages + (int64_t(__builtin_amdgcn_readlane(page, j)) * v.H + h) * size_t(P::BYTES), c16, g);
+            old[to] = *(past && token < past_end ? past + token : reinterpret_cast<const float *>(v.pages));
         };
         const auto compute = [&](int which) {
             uint4_t k[4][KW];
@@ -248,7 +260,7 @@ __global__ __launch_bounds__(256) void fp4_weights_kernel(Fp4Weights a, int page
             }
             const int token = t0 + lane;
             const float all = token_sum(sum, g);
-            if (token < mass_end) mass[token] = past && token < past_end ? in[which].old + all : all;
+            if (token < mass_end) mass[token] = past && token < past_end ? old[which] + all : all;
         };
         // every fetch is made, behind the last page that one again
         const auto next = [&]() {
@@ -271,28 +283,31 @@ __global__ __launch_bounds__(256) void fp4_weights_kernel(Fp4Weights a, int page
 
 // Many columns: a wave keeps the operands of a page, the columns pass through LDS, 64 at a time, in two buffers in turn.
 template <int HD, bool BF16>
-__global__ __launch_bounds__(256) void fp4_weights_tile_kernel(Fp4Weights a, int page_groups) {
+__global__ __launch_bounds__(256, 3) void fp4_weights_tile_kernel(Fp4Weights a, int page_groups) {
     using P = Fp4Block<HD>;
     constexpr int KW = HD / 32;
     __shared__ uint4_t staged[2][4][KW][64];
     __shared__ Fp4RowSet sets[2][4];
     const Fp4View &v = a.v;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c16 = lane & 15, g = lane >> 4;
-    const int h = blockIdx.x % uint32_t(v.H), b = blockIdx.y;
+    const int h = blockIdx.x % uint32_t(v.H), b = blockIdx.y, split = blockIdx.z;
     const Fp4Sequence seq(v, b);
-    const int columns = seq.n * v.G, table_end = (seq.held + FP4_PAGE - 1) / FP4_PAGE;
+    const int table_end = (seq.held + FP4_PAGE - 1) / FP4_PAGE;
     const float *past = a.past ? a.past + (int64_t(b) * v.H + h) * a.pitch : nullptr;
     float *mass = a.mass + (int64_t(b) * v.H + h) * a.pitch;
     const int past_end = int(min(int64_t(min(seq.held, seq.pos0)), a.pitch)), mass_end = int(min(int64_t(seq.held), a.pitch));
+    const int rows64 = 64 / v.G, heads64 = 64 % v.G;
     for (int group = int(blockIdx.x / uint32_t(v.H)); 4 * group < table_end; group += page_groups) {
         const int index = 4 * group + wave, t0 = index * FP4_PAGE, token = t0 + lane;
         const Fp4RowsOf lowest(a, seq, 4 * group * FP4_PAGE), highest(a, seq, (4 * group + 3) * FP4_PAGE);
         const int row0 = lowest.first, row_end = max(lowest.end, highest.end);
-        const int column0 = row0 * v.G / 64 * 64, column_end = row_end * v.G;
+        // the split's columns, 64 at a time
+        const int from = row0 * v.G / 64, stages = (row_end * v.G + 63) / 64 - from, each = (max(stages, 0) + a.splits - 1) / a.splits;
+        const int column0 = 64 * (from + min(each * split, max(stages, 0)));
+        const int column_end = 64 * (from + min(each * (split + 1), max(stages, 0)));
         const int64_t page = index < table_end ? seq.page(v, index) : -1;
         Fp4KPage<HD> in;
-        in.load(v.pages + (max(page, int64_t(0)) * v.H + h) * size_t(P::BYTES),
-                past && token < past_end ? past + token : reinterpret_cast<const float *>(v.pages), c16, g);
+        in.load(v.pages + (max(page, int64_t(0)) * v.H + h) * size_t(P::BYTES), c16, g);
         uint4_t k[4][KW];
         in.template operands<BF16>(k);
         float sum[4] = {0, 0, 0, 0};
@@ -301,17 +316,18 @@ __global__ __launch_bounds__(256) void fp4_weights_tile_kernel(Fp4Weights a, int
             cols.settle(a);
 #pragma unroll
             for (int i = 0; i < KW; ++i) staged[to][wave][i][lane] = cols.q[i];
-            cols.store(sets[to][wave], lane);
+            cols.store(sets[to][wave], seq, lane);
         };
         if (column0 < column_end) {
-            cols.load(a, seq, h, column0 + 16 * wave, columns, lane);
+            cols.start(a, column0 + 16 * wave, lane);
+            cols.load(a, seq, h, lane);
             store(0);
         }
         __syncthreads();
         int now = 0;
         for (int column = column0; column < column_end; column += 64, now ^= 1) {
-            // (behind the last ones those again, which nobody reads)
-            cols.load(a, seq, h, min(column + 64, (column_end - 1) / 64 * 64) + 16 * wave, columns, lane);
+            cols.advance(v.G, rows64, heads64);              // (behind the last ones some more, which nobody reads)
+            cols.load(a, seq, h, lane);
             const int first_hi = __builtin_amdgcn_readfirstlane(sets[now][0].first_hi), last_hi = __builtin_amdgcn_readfirstlane(sets[now][3].last_hi);
             float part[4] = {0, 0, 0, 0};
             const uint4_t(*tile)[KW][64] = staged[now];
@@ -328,7 +344,14 @@ __global__ __launch_bounds__(256) void fp4_weights_tile_kernel(Fp4Weights a, int
                         for (int i = 0; i < KW; ++i) q[(n + 1) & 1][i] = tile[n + 1][i][lane];
                     }
                     scores<HD, BF16>(q[n & 1], k, s[n & 1]);
-                    if (n > 0) weigh_whole<4>(a, s[(n - 1) & 1], sets[now][n - 1].less[g], part);
+                    if (n > 0) {
+                        weigh_whole<4>(a, s[(n - 1) & 1], sets[now][n - 1].less[g], part);
+#pragma unroll
+                        for (int i = 0; i < 4 * KW; ++i) {   // a product, then what fits beside it
+                            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                            __builtin_amdgcn_sched_group_barrier(0x002, 12 / KW, 0);
+                        }
+                    }
                 }
                 weigh_whole<4>(a, s[1], sets[now][3].less[g], part);
             } else {
@@ -347,23 +370,50 @@ __global__ __launch_bounds__(256) void fp4_weights_tile_kernel(Fp4Weights a, int
             __syncthreads();
         }
         const float all = token_sum(sum, g);
-        if (token < mass_end) mass[token] = past && token < past_end ? in.old + all : all;
+        if (a.part) {
+            if (token < mass_end) a.part[((int64_t(split) * v.batch.batch + b) * v.H + h) * (int64_t(v.batch.table_pages) * FP4_PAGE) + token] = all;
+        } else {
+            if (token < mass_end) mass[token] = past && token < past_end ? past[token] + all : all;
+        }
+    }
+}
+
+// Joins the splits, a thread to a token.
+__global__ __launch_bounds__(256) void fp4_weights_join_kernel(Fp4Weights a, int page_groups) {
+    const Fp4View &v = a.v;
+    const int h = blockIdx.x % uint32_t(v.H), b = blockIdx.y;
+    const Fp4Sequence seq(v, b);
+    const int past_end = int(min(int64_t(min(seq.held, seq.pos0)), a.pitch)), mass_end = int(min(int64_t(seq.held), a.pitch));
+    const int64_t stream = int64_t(b) * v.H + h, room = int64_t(v.batch.table_pages) * FP4_PAGE, pitch = room * v.H * v.batch.batch;
+    for (int64_t token = int64_t(blockIdx.x / uint32_t(v.H)) * 256 + threadIdx.x; token < mass_end; token += 256 * int64_t(page_groups)) {
+        const float *part = a.part + stream * room + token;
+        float sum = a.past && token < past_end ? a.past[stream * a.pitch + token] : 0.0f;
+        float all = 0.0f;
+        for (int i = 0; i < a.splits; ++i) all += part[i * pitch];
+        a.mass[stream * a.pitch + token] = sum + all;
     }
 }
 
 // Waves that a call is spread over before a wave takes several pages.
 constexpr int64_t WEIGHTS_WAVES = 8192;
+// Workgroups that many columns are split into.
+constexpr int64_t WEIGHTS_GROUPS = 2304;
 
 int launch_fp4_weights(const kv_fp4_cache *c, const Fp4View &v, const void *q, int64_t q_stride, bool bf16, float sm_scale, int window,
                        int sinks, const float *lse, const float *past, float *mass, int64_t mass_tokens, hipStream_t s) {
-    const Fp4Weights a{v, static_cast<const uint16_t *>(q), q_stride, lse, Fp4Scale::of(sm_scale * FP4_LOG2E), window, sinks,
-                       past, mass, mass_tokens};
+    Fp4Weights a{v, static_cast<const uint16_t *>(q), q_stride, lse, sm_scale * FP4_LOG2E, window, sinks,
+                       past, mass, mass_tokens, nullptr, 1};
     const int64_t columns = int64_t(v.batch.max_new) * v.G, most = int64_t(v.batch.table_pages) * v.H * v.batch.batch;   // pages
     const bool tiles = columns > 16 * WEIGHTS_HELD;
     const int each = tiles ? 1 : int(std::min<int64_t>(std::max<int64_t>(most / WEIGHTS_WAVES, 1), 16));
     const int64_t groups = std::min<int64_t>((v.batch.table_pages + 4 * each - 1) / (4 * each), 4096);
     if (groups * v.H > FP4_GROUPS_MOST) return KV_ERR_UNSUPPORTED;
-    const dim3 grid = dim3(uint32_t(groups * v.H), uint32_t(v.batch.batch));
+    if (tiles) {
+        const int64_t room = FP4_PART_ROWS * (c->cfg.head_dim + 4) / (most * FP4_PAGE), stages = (columns + 63) / 64;
+        a.splits = int(std::max<int64_t>(std::min({WEIGHTS_GROUPS / (groups * v.H * v.batch.batch), room, stages / 4, int64_t(64)}), 1));
+        if (a.splits > 1) a.part = c->workspace + FP4_COUNTERS / sizeof(float);
+    }
+    const dim3 grid = dim3(uint32_t(groups * v.H), uint32_t(v.batch.batch), uint32_t(a.splits));
 #define LAUNCH(HD, BF)                                                                                                              \
     do {                                                                                                                            \
         if (tiles) hipLaunchKernelGGL((fp4_weights_tile_kernel<HD, BF>), grid, dim3(256), 0, s, a, int(groups));                    \
@@ -379,6 +429,10 @@ int launch_fp4_weights(const kv_fp4_cache *c, const Fp4View &v, const void *q, i
     }
 #undef LAUNCH
     KV_HIP_CHECK(hipGetLastError());
+    if (a.part) {
+        hipLaunchKernelGGL(fp4_weights_join_kernel, dim3(uint32_t(groups * v.H), uint32_t(v.batch.batch)), dim3(256), 0, s, a, int(groups));
+        KV_HIP_CHECK(hipGetLastError());
+    }
     return KV_OK;
 }
 
