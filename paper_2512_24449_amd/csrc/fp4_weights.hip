@@ -96,7 +96,7 @@ struct Fp4KPage {
             const int token = 16 * t + c16;
             const uint8_t *from = block + P::K + token * (HD / 2) + g * (HD / 8);
             if constexpr (KW == 4) {
-                const uint4 x = *reinterpret_cast<const uint4 *>(from);
+                const uint4_t x = *reinterpret_cast<const uint4_t *>(from);
                 k[t][0] = x.x, k[t][1] = x.y, k[t][2] = x.z, k[t][3] = x.w;
             } else {
                 const uint2 x = *reinterpret_cast<const uint2 *>(from);
@@ -122,6 +122,16 @@ __device__ inline void scores(const uint4_t (&q)[HD / 32], const uint4_t (&k)[4]
     for (int i = 0; i < HD / 32; ++i)
 #pragma unroll
         for (int t = 0; t < 4; ++t) s[t] = product16<BF16>(q[i], k[t][i], s[t]);
+}
+
+// Products and exponentials of the code before in turn: the matrix core works beside the vector instructions then.
+template <int KW>
+__device__ inline void interleave() {
+#pragma unroll
+    for (int i = 0; i < 4 * KW; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 12 / KW, 0);
+    }
 }
 
 // Adds the weights that 16 columns give to the page's tokens, all of which they see.  NI: registers of a result that hold columns.
@@ -195,7 +205,7 @@ __global__ __launch_bounds__(256) void fp4_weights_kernel(Fp4Weights a, int page
     const int h = blockIdx.x % uint32_t(v.H), b = blockIdx.y;
     int group = int(blockIdx.x / uint32_t(v.H));
     const Fp4Sequence seq(v, b);
-    const int columns = seq.n * v.G, blocks = (columns + 15) / 16;
+    const int columns = seq.n * v.G, blocks = (columns + 31) / 32 * 2;
     const int table_end = (seq.held + FP4_PAGE - 1) / FP4_PAGE;
     if (4 * pages_of_wave * group >= table_end) return;
     Fp4Columns<HD, BF16> cols;
@@ -244,23 +254,46 @@ __global__ __launch_bounds__(256) void fp4_weights_kernel(Fp4Weights a, int page
             in[which].template operands<BF16>(k);
             const int t0 = at[which] * FP4_PAGE;
             float sum[4] = {0, 0, 0, 0};
-            float4_t s[4];
             const bool whole = sees_whole(a, t0, seq.held, max(seq.pos0, -1), max(seq.pos0 + seq.n - 1, -1));   // (wave-uniform)
-            for (int n = 0; n < (ONE ? 1 : blocks); ++n) {
-                if constexpr (ONE) {
-                    scores<HD, BF16>(cols.q, k, s);
-                } else {
+            if constexpr (ONE) {
+                float4_t s[4];
+                scores<HD, BF16>(cols.q, k, s);
+                if (whole) weigh_whole<NI>(a, s, sets[0].less[g], sum);
+                else weigh_some<NI>(a, s, sets[0].less[g], sets[0].hi[g], t0, seq.held, c16, sum);
+            } else if (whole) {
+                // two blocks in turn: the products of one beside the exponentials of the other
+                float4_t s[2][4];
+                uint4_t q[2][KW];
+                const auto operand = [&](int to, int n) {
+#pragma unroll
+                    for (int i = 0; i < KW; ++i) q[to][i] = held[n][i][lane];
+                };
+                operand(0, 0);
+                operand(1, 1);
+                scores<HD, BF16>(q[0], k, s[0]);
+                for (int n = 0; n < blocks; n += 2) {
+                    operand(0, min(n + 2, blocks - 1));
+                    scores<HD, BF16>(q[1], k, s[1]);
+                    weigh_whole<NI>(a, s[0], sets[n].less[g], sum);
+                    interleave<KW>();
+                    operand(1, min(n + 3, blocks - 1));
+                    scores<HD, BF16>(q[0], k, s[0]);         // (behind the last one that one again)
+                    weigh_whole<NI>(a, s[1], sets[n + 1].less[g], sum);
+                    interleave<KW>();
+                }
+            } else {
+                for (int n = 0; n < blocks; ++n) {
                     uint4_t q[KW];
+                    float4_t s[4];
 #pragma unroll
                     for (int i = 0; i < KW; ++i) q[i] = held[n][i][lane];
                     scores<HD, BF16>(q, k, s);
+                    weigh_some<NI>(a, s, sets[n].less[g], sets[n].hi[g], t0, seq.held, c16, sum);
                 }
-                if (whole) weigh_whole<NI>(a, s, sets[n].less[g], sum);
-                else weigh_some<NI>(a, s, sets[n].less[g], sets[n].hi[g], t0, seq.held, c16, sum);
             }
             const int token = t0 + lane;
             const float all = token_sum(sum, g);
-            if (token < mass_end) mass[token] = past && token < past_end ? old[which] + all : all;
+            if (token < mass_end) __builtin_nontemporal_store(past && token < past_end ? old[which] + all : all, mass + token);
         };
         // every fetch is made, behind the last page that one again
         const auto next = [&]() {
@@ -346,11 +379,7 @@ __global__ __launch_bounds__(256, 3) void fp4_weights_tile_kernel(Fp4Weights a, 
                     scores<HD, BF16>(q[n & 1], k, s[n & 1]);
                     if (n > 0) {
                         weigh_whole<4>(a, s[(n - 1) & 1], sets[now][n - 1].less[g], part);
-#pragma unroll
-                        for (int i = 0; i < 4 * KW; ++i) {   // a product, then what fits beside it
-                            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                            __builtin_amdgcn_sched_group_barrier(0x002, 12 / KW, 0);
-                        }
+                        interleave<KW>();
                     }
                 }
                 weigh_whole<4>(a, s[1], sets[now][3].less[g], part);
@@ -394,8 +423,10 @@ __global__ __launch_bounds__(256) void fp4_weights_join_kernel(Fp4Weights a, int
     }
 }
 
-// Waves that a call is spread over before a wave takes several pages.
-constexpr int64_t WEIGHTS_WAVES = 8192;
+// Pages of a wave: one to each of so many waves first (two workgroups to a compute unit).  With more columns than 16 no more
+// waves than these, so that each operand is fetched and laid out as seldom as may be; else up to so many pages.
+constexpr int64_t WEIGHTS_ROUND = 2048;
+constexpr int WEIGHTS_PAGES = 6;
 // Workgroups that many columns are split into.
 constexpr int64_t WEIGHTS_GROUPS = 2304;
 
@@ -405,7 +436,8 @@ int launch_fp4_weights(const kv_fp4_cache *c, const Fp4View &v, const void *q, i
                        past, mass, mass_tokens, nullptr, 1};
     const int64_t columns = int64_t(v.batch.max_new) * v.G, most = int64_t(v.batch.table_pages) * v.H * v.batch.batch;   // pages
     const bool tiles = columns > 16 * WEIGHTS_HELD;
-    const int each = tiles ? 1 : int(std::min<int64_t>(std::max<int64_t>(most / WEIGHTS_WAVES, 1), 16));
+    const int each = tiles ? 1 : int(std::max<int64_t>(columns > 16 ? std::min<int64_t>((most + WEIGHTS_ROUND - 1) / WEIGHTS_ROUND, 64)
+                                                                    : std::min<int64_t>(most / WEIGHTS_ROUND, WEIGHTS_PAGES), 1));
     const int64_t groups = std::min<int64_t>((v.batch.table_pages + 4 * each - 1) / (4 * each), 4096);
     if (groups * v.H > FP4_GROUPS_MOST) return KV_ERR_UNSUPPORTED;
     if (tiles) {
