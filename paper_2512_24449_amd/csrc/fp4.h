@@ -38,6 +38,11 @@ __device__ inline uint32_t max16(uint32_t a, uint32_t b) {
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2_t, a), __builtin_bit_cast(ushort2_t, b)));
 }
 
+// The workspace: a counter byte for each of so many (stream, sequence) pairs whose splits are joined by the last workgroup
+// of them, and partial results, at most so many rows (of a column in a split) of HD + 4 floats.
+constexpr int FP4_COUNTERS = 4096;
+constexpr int64_t FP4_PART_ROWS = 65536;
+
 // What a kernel needs to know of the cache and the batch.
 struct Fp4View {
     uint8_t *pages;

@@ -38,10 +38,6 @@ constexpr float P_LIFT = 12.0f, P_SLACK = 3.0f;
 // s * scale + (P_LIFT - m * scale), whose bracket is rounded to 2^-13 at most; beyond, where that rounding would come to be whole powers
 // of two, from the score: (s - m) * scale + P_LIFT, for the waves that have such a column.
 constexpr float P_FAR = 2048.0f;
-// The workspace: a counter byte for each of so many (stream, sequence) pairs whose splits are joined by the last workgroup
-// of them, and partial results, at most so many rows (of a column in a split) of HD + 4 floats.
-constexpr int FP4_COUNTERS = 4096;
-constexpr int64_t FP4_PART_ROWS = 65536;
 constexpr int FP4_SPLITS_MAX = 256;
 // Sequences that share workgroups by their lengths.
 constexpr int FP4_FLAT = 64;

@@ -13,6 +13,8 @@ struct Fp4Select {
     int keep, sinks, recent;
     const int32_t *budgets;
     int32_t *kept, *n_kept;
+    uint32_t *space;         // of sequences in parts
+    int parts;
 };
 
 // Ordered like the weights: unsigned numbers, the two zeros equal, a NaN above all.
@@ -22,95 +24,332 @@ __device__ inline uint32_t mass_key(float x) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// A workgroup to a (sequence, kv-head).  The weight below which nothing is kept is found digit by digit (11, 11 and 10 bits) by
-// counting keys with the digits found so far; then every wave counts what it has above it and equal to it in a sixteenth of the
-// tokens, and writes its positions behind those of the waves before it.
-constexpr int SELECT_THREADS = 1024, SELECT_WAVES = SELECT_THREADS / 64;
+// The weight below which nothing is kept is found digit by digit (11, 11 and 10 bits of its key) by counting keys with the digits
+// found so far; of the tokens with that weight the first are kept.
+constexpr int SELECT_THREADS = 1024, SELECT_WAVES = SELECT_THREADS / 64, SELECT_BINS = 2048;
+__device__ constexpr int select_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
+__device__ constexpr int select_bins(int pass) { return pass == 2 ? 1024 : 2048; }
 
-__global__ __launch_bounds__(SELECT_THREADS) void fp4_select_kernel(Fp4Select a) {
-    __shared__ uint32_t bins[2048];
+// A sequence's part of a call.
+struct SelectRange {
+    int len, budget, n, begin, end, wanted;   // wanted: of the tokens begin .. end - 1, whose weights decide
+    __device__ inline SelectRange(const Fp4Select &a, const Fp4Sequence &seq, int b) {
+        len = seq.held, budget = min(a.budgets ? max(a.budgets[b], 0) : a.keep, a.keep), n = min(len, budget);
+        const int sinks = min(a.sinks, budget), recent = min(a.recent, budget - sinks);
+        begin = sinks, end = len - recent, wanted = budget - sinks - recent;
+    }
+};
+
+// Counts keys: one in a bin that many lanes share is counted for all of them.
+__device__ inline void count_key(uint32_t *bins, uint32_t bin, bool counts) {
+    const uint64_t all = __ballot(counts);
+    if (!all) return;
+    const uint32_t first = __builtin_amdgcn_readlane(bin, __builtin_ctzll(all));
+    const uint64_t same = __ballot(counts && bin == first);
+    if (counts && bin != first) atomicAdd(&bins[bin], 1u);
+    if ((threadIdx.x & 63) == 0) atomicAdd(&bins[first], uint32_t(__popcll(same)));
+}
+
+// The bin from the top in which the wanted-th key is, and how many are above it.  The thread has bins 2047 - 2 tid and 2046 - 2 tid;
+// all threads call, found and part are LDS.  Contains two barriers.
+struct SelectBin {
+    uint32_t bin, above;
+};
+__device__ inline SelectBin find_bin(uint32_t hi, uint32_t lo, uint32_t wanted, uint32_t *part, uint32_t *found) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const uint32_t upto = uint32_t(wave_inclusive_scan(int(hi + lo)));
+    if (lane == 63) part[wave] = upto;
+    __syncthreads();
+    const uint32_t waves = uint32_t(wave_inclusive_scan(lane < SELECT_WAVES ? int(part[lane]) : 0));
+    const uint32_t before = upto - hi - lo + (wave ? __builtin_amdgcn_readlane(waves, (wave - 1) & 63) : 0u);
+    if (before < wanted && wanted <= before + hi + lo) {
+        const bool in_hi = wanted <= before + hi;
+        found[0] = uint32_t(in_hi ? 2047 - 2 * tid : 2046 - 2 * tid);
+        found[1] = in_hi ? before : before + hi;
+    }
+    __syncthreads();
+    return {found[0], found[1]};
+}
+
+// Writes the positions of what is kept of 64 tokens, in order: those that are sure, and of the tied ones as many as are still wanted.
+__device__ inline void write_kept(int32_t *kept, int t, bool sure, bool tie, uint32_t wanted, uint32_t &at, uint32_t &tied, int lane) {
+    const uint64_t lower = (uint64_t(1) << lane) - 1, ties = __ballot(tie);
+    const bool mine = sure || (tie && tied + uint32_t(__popcll(ties & lower)) < wanted);
+    const uint64_t keeps = __ballot(mine);
+    if (mine) kept[at + uint32_t(__popcll(keeps & lower))] = t;
+    at += uint32_t(__popcll(keeps)), tied += uint32_t(__popcll(ties));
+}
+
+// A workgroup to a (sequence, kv-head), a wave to a sixteenth of the tokens.  KEYS: rounds of a wave whose keys stay in registers; 0: any
+// number, the keys are read again for every digit.
+template <int KEYS>
+__global__ __launch_bounds__(SELECT_THREADS, 8) void fp4_select_kernel(Fp4Select a) {
+    __shared__ uint32_t bins[SELECT_BINS];
     __shared__ uint32_t found[2], part[SELECT_WAVES], above[SELECT_WAVES], equal[SELECT_WAVES];
     const Fp4View &v = a.v;
-    const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Fp4Sequence seq(v, b);
+    const SelectRange r(a, seq, b);
     const int64_t stream = int64_t(b) * v.H + h;
     const float *mass = a.mass + stream * a.pitch;
     int32_t *kept = a.kept + stream * a.keep;
-    const int len = seq.held, budget = min(a.budgets ? max(a.budgets[b], 0) : a.keep, a.keep), n = min(len, budget);
-    if (h == 0 && tid == 0) a.n_kept[b] = n;
-    for (int i = n + tid; i < a.keep; i += SELECT_THREADS) kept[i] = -1;
-    if (len <= budget) {
-        for (int i = tid; i < n; i += SELECT_THREADS) kept[i] = i;
+    if (h == 0 && tid == 0) a.n_kept[b] = r.n;
+    for (int i = r.n + tid; i < a.keep; i += SELECT_THREADS) kept[i] = -1;
+    if (r.len <= r.budget) {
+        for (int i = tid; i < r.n; i += SELECT_THREADS) kept[i] = i;
         return;
     }
-    const int sinks = min(a.sinks, budget), recent = min(a.recent, budget - sinks), begin = sinks, end = len - recent;
-    int wanted = budget - sinks - recent;              // of begin .. end - 1
-    const auto key = [&](int t) { return mass_key(t < a.pitch ? mass[t] : 0.0f); };
-    uint32_t digits = 0, mask = 0;                     // of the key that is looked for, and which are known
-    if (wanted > 0) {
-        for (int pass = 0; pass < 3; ++pass) {
-            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, count = pass == 2 ? 1024 : 2048;
-            for (int i = tid; i < 2048; i += SELECT_THREADS) bins[i] = 0;
-            __syncthreads();
-            for (int t = begin + tid; t < end; t += SELECT_THREADS) {
-                const uint32_t x = key(t);
-                if (((x ^ digits) & mask) == 0) atomicAdd(&bins[(x >> shift) & (count - 1)], 1u);
-            }
-            __syncthreads();
-            // bins from the top: two to a thread, thread 0 the highest
-            const uint32_t hi = bins[2047 - 2 * tid], lo = bins[2046 - 2 * tid];
-            const uint32_t upto = uint32_t(wave_inclusive_scan(int(hi + lo)));
-            if (lane == 63) part[wave] = upto;
-            __syncthreads();
-            uint32_t before = upto - hi - lo;
-            for (int w = 0; w < wave; ++w) before += part[w];
-            if (before < uint32_t(wanted) && uint32_t(wanted) <= before + hi + lo) {
-                const bool in_hi = uint32_t(wanted) <= before + hi;
-                found[0] = uint32_t(in_hi ? 2047 - 2 * tid : 2046 - 2 * tid);
-                found[1] = in_hi ? before : before + hi;
-            }
-            __syncthreads();
-            digits |= found[0] << shift, mask |= uint32_t(count - 1) << shift;
-            wanted -= int(found[1]);                   // still wanted of those with these digits
-            __syncthreads();
-        }
-    } else {
-        digits = 0xFFFFFFFFu;
-        wanted = 0;
+    const int rounds = ((r.len + SELECT_WAVES - 1) / SELECT_WAVES + 63) / 64, from = wave * rounds * 64;
+    const int upto = int(min(int64_t(r.end), a.pitch));          // (tokens without a place have weight 0)
+    const auto read = [&](int t) { return t < upto ? mass[t] : 0.0f; };
+    uint32_t held[KEYS ? KEYS : 1];
+    if constexpr (KEYS > 0) {
+        float x[KEYS];
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) x[i] = i < rounds ? read(from + 64 * i + lane) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) held[i] = mass_key(x[i]);
     }
-    // a wave's tokens: a sixteenth of all, in order
-    const bool some = budget - sinks - recent > 0;
-    const int each = ((len + SELECT_WAVES - 1) / SELECT_WAVES + 63) & ~63, from = min(wave * each, len), to = min(from + each, len);
-    const auto classify = [&](int t, bool &sure, bool &tie) {
-        sure = tie = false;
-        if (t >= to) return;
-        if (t < begin || t >= end) sure = true;
-        else if (some) {
-            const uint32_t x = key(t);
-            sure = x > digits, tie = x == digits;
+    // f(position, key) for every round of the wave
+    const auto each = [&](auto f) {
+        if constexpr (KEYS > 0) {
+            int t = from + lane;
+#pragma unroll
+            for (int i = 0; i < KEYS; ++i) {
+                asm volatile("" : "+v"(t));      // (found again every time: positions kept for all rounds would cost as many registers)
+                if (i < rounds) f(t, held[i]);
+                t += 64;
+            }
+        } else {
+            for (int i = 0; i < rounds; ++i) f(from + 64 * i + lane, mass_key(read(from + 64 * i + lane)));
         }
     };
-    uint32_t sures = 0, ties = 0;
-    for (int t0 = from; t0 < to; t0 += 64) {
-        bool sure, tie;
-        classify(t0 + lane, sure, tie);
-        sures += uint32_t(__popcll(__ballot(sure))), ties += uint32_t(__popcll(__ballot(tie)));
+    uint32_t digits = 0, mask = 0, wanted = uint32_t(max(r.wanted, 0));   // of the key that is looked for, and which are known
+    const bool some = wanted > 0;
+    for (int pass = 0; some && pass < 3; ++pass) {
+        for (int i = tid; i < SELECT_BINS; i += SELECT_THREADS) bins[i] = 0;
+        __syncthreads();
+        const int shift = select_shift(pass), count = select_bins(pass);
+        each([&](int t, uint32_t key) { count_key(bins, (key >> shift) & (count - 1), t >= r.begin && t < r.end && ((key ^ digits) & mask) == 0); });
+        __syncthreads();
+        const SelectBin x = find_bin(bins[2047 - 2 * tid], bins[2046 - 2 * tid], wanted, part, found);
+        digits |= x.bin << shift, mask |= uint32_t(count - 1) << shift;
+        wanted -= x.above;                                       // still wanted of those with these digits
+        __syncthreads();
     }
+    const auto sure = [&](int t, uint32_t key) { return t < r.len && (t < r.begin || t >= r.end || (some && key > digits)); };
+    const auto tie = [&](int t, uint32_t key) { return some && t >= r.begin && t < r.end && key == digits; };
+    uint32_t sures = 0, ties = 0;
+    each([&](int t, uint32_t key) { sures += uint32_t(__popcll(__ballot(sure(t, key)))), ties += uint32_t(__popcll(__ballot(tie(t, key)))); });
     if (lane == 0) above[wave] = sures, equal[wave] = ties;
     __syncthreads();
-    uint32_t at = 0, tied = 0;                         // kept and tied of the waves before
-    for (int w = 0; w < wave; ++w) at += above[w], tied += equal[w];
-    at += min(tied, uint32_t(wanted));
-    const uint64_t lower = (uint64_t(1) << lane) - 1;
-    for (int t0 = from; t0 < to; t0 += 64) {
-        bool sure, tie;
-        classify(t0 + lane, sure, tie);
-        const uint64_t tie_mask = __ballot(tie);
-        const bool mine = sure || (tie && tied + uint32_t(__popcll(tie_mask & lower)) < uint32_t(wanted));
-        const uint64_t keep_mask = __ballot(mine);
-        if (mine) kept[at + uint32_t(__popcll(keep_mask & lower))] = t0 + lane;
-        at += uint32_t(__popcll(keep_mask)), tied += uint32_t(__popcll(tie_mask));
+    uint32_t at = uint32_t(wave_inclusive_scan(lane < wave ? int(above[lane]) : 0)), tied = uint32_t(wave_inclusive_scan(lane < wave ? int(equal[lane]) : 0));
+    at = __builtin_amdgcn_readlane(at, 63), tied = __builtin_amdgcn_readlane(tied, 63);   // of the waves before
+    at += min(tied, wanted);
+    each([&](int t, uint32_t key) { write_kept(kept, t, sure(t, key), tie(t, key), wanted, at, tied, lane); });
+}
+
+// Long sequences of few heads, a workgroup to SELECT_PART tokens, in three launches: counts of the first digit of every part; that
+// digit from all parts' counts, and each part's keys with it; the other digits from those keys -- every workgroup for
+// itself -- and the positions.  What the parts hand on of a (sequence, kv-head): counts [parts][2048], keys
+// [parts][SELECT_PART], tokens above the digit [parts] and keys [parts], the digit and how many are wanted of it.
+constexpr int SELECT_ROUNDS = 8, SELECT_PART = SELECT_ROUNDS * SELECT_THREADS, SELECT_LISTED = 12288, SELECT_PARTS = 256;
+
+struct SelectSpace {
+    uint32_t *counts, *keys, *above, *listed, *digit;
+    static __host__ __device__ inline int64_t words(int parts) { return int64_t(parts) * (SELECT_BINS + SELECT_PART + 2) + 2; }
+    __device__ inline SelectSpace(const Fp4Select &a, int64_t stream) {
+        counts = a.space + stream * words(a.parts);
+        keys = counts + int64_t(a.parts) * SELECT_BINS;
+        above = keys + int64_t(a.parts) * SELECT_PART;
+        listed = above + a.parts;
+        digit = listed + a.parts;
     }
+};
+
+// A part's keys, wave by wave in order.
+struct SelectPart {
+    float held[SELECT_ROUNDS];
+    int from;
+    __device__ inline void load(const float *mass, int upto, int part, int wave, int lane) {
+        from = part * SELECT_PART + wave * (64 * SELECT_ROUNDS) + lane;
+#pragma unroll
+        for (int i = 0; i < SELECT_ROUNDS; ++i) held[i] = from + 64 * i < upto ? mass[from + 64 * i] : 0.0f;
+    }
+    template <class F>
+    __device__ inline void each(F f) const {
+#pragma unroll
+        for (int i = 0; i < SELECT_ROUNDS; ++i) f(from + 64 * i, mass_key(held[i]));
+    }
+};
+
+template <int STEP>
+__global__ __launch_bounds__(SELECT_THREADS) void fp4_select_part_kernel(Fp4Select a) {
+    __shared__ uint32_t bins[SELECT_BINS];
+    __shared__ uint32_t found[2], part_sums[SELECT_WAVES], above[SELECT_WAVES], equal[SELECT_WAVES];
+    __shared__ uint32_t list[STEP == 2 ? SELECT_LISTED : 1], starts[STEP == 2 ? SELECT_PARTS + 1 : 1];
+    const Fp4View &v = a.v;
+    const int h = blockIdx.x % uint32_t(v.H), part = int(blockIdx.x / uint32_t(v.H)), b = blockIdx.y;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Fp4Sequence seq(v, b);
+    const SelectRange r(a, seq, b);
+    const int64_t stream = int64_t(b) * v.H + h;
+    int32_t *kept = a.kept + stream * a.keep;
+    if (STEP == 2) {
+        if (h == 0 && part == 0 && tid == 0) a.n_kept[b] = r.n;
+        for (int64_t i = r.n + int64_t(part) * SELECT_THREADS + tid; i < a.keep; i += int64_t(a.parts) * SELECT_THREADS) kept[i] = -1;
+    }
+    if (part * SELECT_PART >= r.len) return;
+    if (r.len <= r.budget) {
+        if (STEP == 2)
+            for (int i = part * SELECT_PART + tid; i < min(r.n, (part + 1) * SELECT_PART); i += SELECT_THREADS) kept[i] = i;
+        return;
+    }
+    const SelectSpace space(a, stream);
+    const int parts = (r.len + SELECT_PART - 1) / SELECT_PART;   // that there are
+    const bool some = r.wanted > 0;
+    if (!some && STEP < 2) return;
+    SelectPart mine;
+    mine.load(a.mass + stream * a.pitch, int(min(int64_t(r.end), a.pitch)), part, wave, lane);
+    const auto decides = [&](int t) { return t >= r.begin && t < r.end; };
+
+    if constexpr (STEP == 0) {
+        for (int i = tid; i < SELECT_BINS; i += SELECT_THREADS) bins[i] = 0;
+        __syncthreads();
+        mine.each([&](int t, uint32_t key) { count_key(bins, key >> 21, decides(t)); });
+        __syncthreads();
+        for (int i = tid; i < SELECT_BINS; i += SELECT_THREADS) space.counts[int64_t(part) * SELECT_BINS + i] = bins[i];
+        return;
+    }
+    if constexpr (STEP == 1) {
+        uint32_t hi = 0, lo = 0;
+#pragma unroll 8
+        for (int i = 0; i < parts; ++i) {
+            const uint2 two = *reinterpret_cast<const uint2 *>(space.counts + int64_t(i) * SELECT_BINS + 2046 - 2 * tid);
+            lo += two.x, hi += two.y;
+        }
+        const SelectBin x = find_bin(hi, lo, uint32_t(r.wanted), part_sums, found);
+        if (part == 0 && tid == 0) space.digit[0] = x.bin, space.digit[1] = uint32_t(r.wanted) - x.above;
+        uint32_t more = 0, same = 0;
+        mine.each([&](int t, uint32_t key) {
+            more += uint32_t(__popcll(__ballot(t < r.len && (!decides(t) || (key >> 21) > x.bin))));
+            same += uint32_t(__popcll(__ballot(decides(t) && (key >> 21) == x.bin)));
+        });
+        if (lane == 0) above[wave] = more, equal[wave] = same;
+        __syncthreads();
+        const uint32_t before = uint32_t(wave_inclusive_scan(lane < SELECT_WAVES ? int(equal[lane]) : 0));
+        const uint32_t sures = uint32_t(wave_inclusive_scan(lane < SELECT_WAVES ? int(above[lane]) : 0));
+        if (tid == 63) space.above[part] = sures, space.listed[part] = before;
+        uint32_t at = wave ? __builtin_amdgcn_readlane(before, (wave - 1) & 63) : 0u;
+        uint32_t *keys = space.keys + int64_t(part) * SELECT_PART;
+        mine.each([&](int t, uint32_t key) {
+            const bool in = decides(t) && (key >> 21) == x.bin;
+            const uint64_t all = __ballot(in);
+            if (in) keys[at + uint32_t(__popcll(all & ((uint64_t(1) << lane) - 1)))] = key;
+            at += uint32_t(__popcll(all));
+        });
+        return;
+    }
+    if constexpr (STEP == 2) {
+        uint32_t digits = 0, wanted = 0, before = 0, tied = 0;   // before, tied: kept for sure and tied in the parts before
+        if (some) {
+            digits = space.digit[0] << 21, wanted = space.digit[1];
+            // where each part's listed keys begin among all, and the keys themselves, in LDS if there is room
+            if (wave == 0) {
+                uint32_t sum = 0;
+                for (int i = 0; i < parts; i += 64) {
+                    const uint32_t n = i + lane < parts ? space.listed[i + lane] : 0u, upto = uint32_t(wave_inclusive_scan(int(n)));
+                    if (i + lane < parts) starts[i + lane] = sum + upto - n;
+                    sum += __builtin_amdgcn_readlane(upto, 63);
+                }
+                if (lane == 0) starts[parts] = sum;
+            }
+            __syncthreads();
+            const uint32_t total = starts[parts], mine_at = starts[part];
+            const bool room = total <= SELECT_LISTED;
+            if (room) {
+                for (int i = wave; i < parts; i += SELECT_WAVES) {
+                    const uint32_t at = starts[i], n = starts[i + 1] - at;
+                    for (uint32_t j = lane; j < n; j += 64) list[at + j] = space.keys[int64_t(i) * SELECT_PART + j];
+                }
+                __syncthreads();
+            }
+            const auto listed = [&](auto f) {                    // f(number among all, key, whether there is one), whole waves
+                if (room) {
+                    for (uint32_t j = 64 * wave; j < total; j += SELECT_THREADS) {
+                        const bool in = j + lane < total;
+                        f(j + lane, in ? list[j + lane] : 0u, in);
+                    }
+                } else {
+                    for (int i = 0; i < parts; ++i) {
+                        const uint32_t at = starts[i], n = starts[i + 1] - at;
+                        for (uint32_t j = 64 * wave; j < n; j += SELECT_THREADS) {
+                            const bool in = j + lane < n;
+                            f(at + j + lane, in ? space.keys[int64_t(i) * SELECT_PART + j + lane] : 0u, in);
+                        }
+                    }
+                }
+            };
+            uint32_t mask = 0xFFFFFFFFu << 21;
+            for (int pass = 1; pass < 3; ++pass) {
+                for (int i = tid; i < SELECT_BINS; i += SELECT_THREADS) bins[i] = 0;
+                __syncthreads();
+                const int shift = select_shift(pass), count = select_bins(pass);
+                listed([&](uint32_t, uint32_t key, bool in) { count_key(bins, (key >> shift) & (count - 1), in && ((key ^ digits) & mask) == 0); });
+                __syncthreads();
+                const SelectBin x = find_bin(bins[2047 - 2 * tid], bins[2046 - 2 * tid], wanted, part_sums, found);
+                digits |= x.bin << shift, mask |= uint32_t(count - 1) << shift;
+                wanted -= x.above;
+                __syncthreads();
+            }
+            uint32_t more = 0, same = 0;
+            listed([&](uint32_t i, uint32_t key, bool in) {
+                more += uint32_t(__popcll(__ballot(in && i < mine_at && key > digits)));
+                same += uint32_t(__popcll(__ballot(in && i < mine_at && key == digits)));
+            });
+            uint32_t sures = 0;
+            for (int i = 64 * wave; i < part; i += SELECT_THREADS) sures += i + lane < part ? space.above[i + lane] : 0u;
+            more += __builtin_amdgcn_readlane(uint32_t(wave_inclusive_scan(int(sures))), 63);
+            if (lane == 0) above[wave] = more, equal[wave] = same;
+            __syncthreads();
+            for (int i = 0; i < SELECT_WAVES; ++i) before += above[i], tied += equal[i];
+            __syncthreads();
+        } else {
+            before = uint32_t(min(part * SELECT_PART, r.begin) + max(part * SELECT_PART - r.end, 0));
+        }
+        const auto sure = [&](int t, uint32_t key) { return t < r.len && (!decides(t) || (some && key > digits)); };
+        const auto tie = [&](int t, uint32_t key) { return some && decides(t) && key == digits; };
+        uint32_t sures = 0, ties = 0;
+        mine.each([&](int t, uint32_t key) { sures += uint32_t(__popcll(__ballot(sure(t, key)))), ties += uint32_t(__popcll(__ballot(tie(t, key)))); });
+        if (lane == 0) above[wave] = sures, equal[wave] = ties;
+        __syncthreads();
+        for (int i = 0; i < wave; ++i) before += above[i], tied += equal[i];
+        uint32_t at = before + min(tied, wanted);
+        mine.each([&](int t, uint32_t key) { write_kept(kept, t, sure(t, key), tie(t, key), wanted, at, tied, lane); });
+    }
+}
+
+int launch_fp4_select(const kv_fp4_cache *c, Fp4Select a, hipStream_t s) {
+    const int64_t room = int64_t(a.v.batch.table_pages) * FP4_PAGE, streams = int64_t(a.v.H) * a.v.batch.batch;
+    a.parts = int((room + SELECT_PART - 1) / SELECT_PART);
+    a.space = reinterpret_cast<uint32_t *>(c->workspace) + FP4_COUNTERS / sizeof(uint32_t);
+    const bool in_parts = room > 32 * SELECT_THREADS && a.parts <= SELECT_PARTS && streams * SelectSpace::words(a.parts) <= FP4_PART_ROWS * (c->cfg.head_dim + 4);
+    if (in_parts) {
+        const dim3 grid = dim3(uint32_t(a.parts * a.v.H), uint32_t(a.v.batch.batch));
+        hipLaunchKernelGGL(fp4_select_part_kernel<0>, grid, dim3(SELECT_THREADS), 0, s, a);
+        KV_HIP_CHECK(hipGetLastError());
+        hipLaunchKernelGGL(fp4_select_part_kernel<1>, grid, dim3(SELECT_THREADS), 0, s, a);
+        KV_HIP_CHECK(hipGetLastError());
+        hipLaunchKernelGGL(fp4_select_part_kernel<2>, grid, dim3(SELECT_THREADS), 0, s, a);
+    } else {
+        const dim3 grid = dim3(uint32_t(a.v.H), uint32_t(a.v.batch.batch));
+        if (room <= 4 * SELECT_THREADS) hipLaunchKernelGGL(fp4_select_kernel<4>, grid, dim3(SELECT_THREADS), 0, s, a);
+        else if (room <= 16 * SELECT_THREADS) hipLaunchKernelGGL(fp4_select_kernel<16>, grid, dim3(SELECT_THREADS), 0, s, a);
+        else if (room <= 32 * SELECT_THREADS) hipLaunchKernelGGL(fp4_select_kernel<32>, grid, dim3(SELECT_THREADS), 0, s, a);
+        else hipLaunchKernelGGL(fp4_select_kernel<0>, grid, dim3(SELECT_THREADS), 0, s, a);
+    }
+    KV_HIP_CHECK(hipGetLastError());
+    return KV_OK;
 }
 
 struct Fp4Compact {
@@ -199,11 +438,8 @@ extern "C" int kv_fp4_select(kv_fp4_cache_t *c, const kv_fp4_batch_t *batch, con
     if (rc) return rc;
     if (mass_tokens < 1 || keep < 1 || sinks < 0 || recent < 0) return KV_ERR_ARG;
     if (!fp4_aligned(mass, 4) || !fp4_aligned(kept, 4) || !fp4_aligned(n_kept, 4) || (budgets && !fp4_aligned(budgets, 4))) return KV_ERR_ARG;
-    const Fp4Select a{fp4_view(c, batch, 0), mass, mass_tokens, keep, sinks, recent, budgets, kept, n_kept};
-    hipLaunchKernelGGL(fp4_select_kernel, dim3(uint32_t(c->cfg.n_kv_heads), uint32_t(batch->batch)), dim3(SELECT_THREADS), 0,
-                       static_cast<hipStream_t>(hip_stream), a);
-    KV_HIP_CHECK(hipGetLastError());
-    return KV_OK;
+    return launch_fp4_select(c, Fp4Select{fp4_view(c, batch, 0), mass, mass_tokens, keep, sinks, recent, budgets, kept, n_kept, nullptr, 0},
+                             static_cast<hipStream_t>(hip_stream));
 }
 
 extern "C" int kv_fp4_compact(kv_fp4_cache_t *c, const kv_fp4_batch_t *from, const kv_fp4_batch_t *to, const int32_t *kept, int32_t keep,

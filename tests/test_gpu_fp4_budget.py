@@ -253,6 +253,35 @@ def test_select_with_budgets_narrow_tensors_and_narrow_tables():
     check_select(m, [-5, 800, 700, 2 ** 31 - 1, 50, 3], 150, 4, 20, table_pages=10)
 
 
+@pytest.mark.parametrize("pages", [600, 1025])
+def test_select_in_long_tables(pages):
+    """Tables of more than 32768 tokens: sequences of all lengths in them, few and many tokens with the decisive weight's first digits."""
+    lens = [64 * pages, 40000, 8192, 8193, 3, 0]
+    m = heavy((6, 1, 64 * pages), 7)
+    check_select(m, lens, 5000, 4, 100, table_pages=pages)
+    check_select(m, lens, 37000, 0, 0, table_pages=pages, budgets=[37000, 36999, 5000, 8193, 0, 9])
+    check_select(m, lens, 3000, 3000, 9, table_pages=pages)
+    check_select(m, lens, 40000, 10000, 20000, table_pages=pages)
+    check_select(m[..., :30000].contiguous(), lens, 20000, 4, 100, table_pages=pages)
+    m = (1.0 + torch.rand(6, 1, 64 * pages, generator=torch.Generator().manual_seed(8)) / 8)      # one first digit for all
+    check_select(m, lens, 20000, 4, 100, table_pages=pages)
+    check_select((m * 64).round() / 64, lens, 20001, 0, 100, table_pages=pages)
+    check_select(torch.zeros(6, 1, 64 * pages), lens, 33333, 1, 1, table_pages=pages)
+
+
+def test_select_of_many_heads_in_long_tables():
+    """More than the workspace takes in parts: a workgroup to a head all the same."""
+    lens, heads = [40000, 100], 300
+    m = heavy((2, heads, 40000), 9)
+    cache = binding.FP4KVCache(1, heads, heads, 64)
+    batch = binding.FP4Batch(ints(lens), 0, table_pages=700)
+    kept, count = cache.kv_fp4_select(m.to(DEV), batch, 1000, 4, 100)
+    assert count.tolist() == [1000, 100]
+    for b, h in ((0, 0), (0, 299), (1, 7), (0, 123)):
+        want = ref.kept(m[b, h].tolist(), lens[b], 1000, 4, 100)
+        assert kept[b, h].tolist() == want + [-1] * (1000 - len(want))
+
+
 # ---- rows moved together ----
 
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
