@@ -1,5 +1,6 @@
 // Which tokens of the 4-bit paged cache are kept, and their rows moved together (packkv.h: kv_fp4_select, kv_fp4_compact).
 #include <algorithm>
+#include <type_traits>
 
 #include "fp4.h"
 #include "unpack.h"
@@ -80,10 +81,138 @@ __device__ inline void write_kept(int32_t *kept, int t, bool sure, bool tie, uin
     at += uint32_t(__popcll(keeps)), tied += uint32_t(__popcll(ties));
 }
 
-// A workgroup to a (sequence, kv-head), a wave to a sixteenth of the tokens.  KEYS: rounds of a wave whose keys stay in registers; 0: any
-// number, the keys are read again for every digit.
+// The threads' numbers of something, up to this thread's (excluded), and of all.  All threads call; sums: LDS.  Contains a barrier.
+__device__ inline uint32_t sum_before(uint32_t mine, uint32_t *sums, uint32_t *all) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t upto = uint32_t(wave_inclusive_scan(int(mine)));
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    const uint32_t waves = uint32_t(wave_inclusive_scan(lane < SELECT_WAVES ? int(sums[lane]) : 0));
+    *all = __builtin_amdgcn_readlane(waves, 63);
+    return upto - mine + (wave ? __builtin_amdgcn_readlane(waves, (__builtin_amdgcn_readfirstlane(wave) - 1) & 63) : 0u);
+}
+
+// A workgroup to a (sequence, kv-head), up to KEYS tokens in a row to a thread, whose keys are read once and stay in registers: which of them
+// are kept is bits of a word, positions come from one sum over the threads.  The keys with the first digit that is found go to LDS
+// and the others are found among them, if there is room.  Bound by vector instructions (some 30 to a token and lane) and LDS.
+constexpr uint32_t KEY_OF_0 = 0x80000000u, KEY_OF_NONE = 0;      // (no number has the key 0)
+constexpr int SELECT_LIST = 4096;
 template <int KEYS>
-__global__ __launch_bounds__(SELECT_THREADS, 8) void fp4_select_kernel(Fp4Select a) {
+__global__ __launch_bounds__(SELECT_THREADS, KEYS > 32 ? 4 : 8) void fp4_select_kernel(Fp4Select a) {
+    using Bits = std::conditional_t<(KEYS > 32), uint64_t, uint32_t>;
+    __shared__ uint32_t bins[SELECT_BINS], list[SELECT_LIST];
+    __shared__ uint32_t found[2], part[SELECT_WAVES], sums[2][SELECT_WAVES];
+    const Fp4View &v = a.v;
+    const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+    const Fp4Sequence seq(v, b);
+    const SelectRange r(a, seq, b);
+    const int64_t stream = int64_t(b) * v.H + h;
+    const float *mass = a.mass + stream * a.pitch;
+    int32_t *kept = a.kept + stream * a.keep;
+    if (h == 0 && tid == 0) a.n_kept[b] = r.n;
+    for (int i = r.n + tid; i < a.keep; i += SELECT_THREADS) kept[i] = -1;
+    if (r.len <= r.budget) {
+        for (int i = tid; i < r.n; i += SELECT_THREADS) kept[i] = i;
+        return;
+    }
+    // this thread's tokens, a multiple of four
+    const int mine = ((r.len + SELECT_THREADS - 1) / SELECT_THREADS + 3) & ~3, t0 = tid * mine;
+    const int upto = int(min(int64_t(r.len), a.pitch));          // (tokens without a place have weight 0)
+    const auto below = [&](int t) {                              // bits of the tokens below position t
+        const int n = min(max(t - t0, 0), mine);
+        return n < int(8 * sizeof(Bits)) ? (Bits(1) << n) - 1 : ~Bits(0);
+    };
+    const Bits decides = r.wanted > 0 ? below(r.end) & ~below(r.begin) : 0;
+    uint32_t key[KEYS];
+    typedef float four_t __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+    for (int i = 0; i < KEYS; i += 4) {
+        float x[4] = {0, 0, 0, 0};
+        if (i < mine) {
+            if (t0 + i + 4 <= upto) {
+                const four_t y = *reinterpret_cast<const four_t *>(mass + t0 + i);
+                x[0] = y[0], x[1] = y[1], x[2] = y[2], x[3] = y[3];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (t0 + i + j < upto) x[j] = mass[t0 + i + j];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) key[i + j] = __float_as_uint(x[j]);
+    }
+#pragma unroll
+    for (int i = 0; i < KEYS; ++i) key[i] = (decides >> i) & 1 ? mass_key(__uint_as_float(key[i])) : KEY_OF_NONE;
+
+    Bits sure = below(r.begin) | (below(r.len) & ~below(r.end)), tie = 0;
+    uint32_t wanted = uint32_t(max(r.wanted, 0));
+    if (wanted > 0) {                                            // (uniform)
+        for (int i = tid; i < SELECT_BINS; i += SELECT_THREADS) bins[i] = 0;
+        __syncthreads();
+        // weights of 0 are many where a window hides tokens: counted for the wave
+        uint32_t zeros = 0;
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) {
+            if (i < mine) {
+                zeros += uint32_t(__popcll(__ballot(key[i] == KEY_OF_0)));
+                if (key[i] << 1) atomicAdd(&bins[key[i] >> select_shift(0)], 1u);
+            }
+        }
+        if (lane == 0 && zeros) atomicAdd(&bins[KEY_OF_0 >> select_shift(0)], zeros);
+        __syncthreads();
+        SelectBin x = find_bin(bins[2047 - 2 * tid], bins[2046 - 2 * tid], wanted, part, found);
+        wanted -= x.above;
+        uint32_t digits = x.bin << select_shift(0), mask = 0xFFFFFFFFu << select_shift(0);
+        Bits in = 0;
+        uint32_t total;
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) in |= Bits(key[i] >> select_shift(0) == x.bin) << i;
+        in &= decides;
+        uint32_t at = sum_before(uint32_t(__popcll(uint64_t(in))), sums[0], &total);
+        const bool listed = total <= SELECT_LIST;
+        if (listed) {
+#pragma unroll
+            for (int i = 0; i < KEYS; ++i)
+                if ((in >> i) & 1) list[at++] = key[i];
+        }
+        for (int pass = 1; pass < 3; ++pass) {
+            const int shift = select_shift(pass), count = select_bins(pass);
+            for (int i = tid; i < SELECT_BINS; i += SELECT_THREADS) bins[i] = 0;
+            __syncthreads();
+            if (listed) {
+                for (uint32_t j = tid - lane; j < total; j += SELECT_THREADS) {
+                    const uint32_t k = j + lane < total ? list[j + lane] : 0u;
+                    count_key(bins, (k >> shift) & (count - 1), j + lane < total && ((k ^ digits) & mask) == 0);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < KEYS; ++i)
+                    if (i < mine) count_key(bins, (key[i] >> shift) & (count - 1), key[i] != KEY_OF_NONE && ((key[i] ^ digits) & mask) == 0);
+            }
+            __syncthreads();
+            x = find_bin(bins[2047 - 2 * tid], bins[2046 - 2 * tid], wanted, part, found);
+            digits |= x.bin << shift, mask |= uint32_t(count - 1) << shift;
+            wanted -= x.above;
+        }
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) sure |= Bits(key[i] > digits) << i, tie |= Bits(key[i] == digits) << i;
+    }
+    // of the tied ones as many as are still wanted, from the front
+    uint32_t all;
+    const uint32_t before = sum_before(uint32_t(__popcll(uint64_t(tie))), sums[1], &all);
+    for (uint32_t n = before < wanted ? wanted - before : 0; n && tie; --n) {
+        sure |= tie & (~tie + 1);
+        tie &= tie - 1;
+    }
+    uint32_t at = sum_before(uint32_t(__popcll(uint64_t(sure))), sums[0], &all);
+    while (sure) {
+        kept[at++] = t0 + __builtin_ctzll(uint64_t(sure));
+        sure &= sure - 1;
+    }
+}
+
+// Any length, of any number of heads: the keys are read again for every digit, a wave's sixteenth of the tokens in order.
+__global__ __launch_bounds__(SELECT_THREADS) void fp4_select_long_kernel(Fp4Select a) {
     __shared__ uint32_t bins[SELECT_BINS];
     __shared__ uint32_t found[2], part[SELECT_WAVES], above[SELECT_WAVES], equal[SELECT_WAVES];
     const Fp4View &v = a.v;
@@ -100,28 +229,11 @@ __global__ __launch_bounds__(SELECT_THREADS, 8) void fp4_select_kernel(Fp4Select
         return;
     }
     const int rounds = ((r.len + SELECT_WAVES - 1) / SELECT_WAVES + 63) / 64, from = wave * rounds * 64;
-    const int upto = int(min(int64_t(r.end), a.pitch));          // (tokens without a place have weight 0)
-    const auto read = [&](int t) { return t < upto ? mass[t] : 0.0f; };
-    uint32_t held[KEYS ? KEYS : 1];
-    if constexpr (KEYS > 0) {
-        float x[KEYS];
-#pragma unroll
-        for (int i = 0; i < KEYS; ++i) x[i] = i < rounds ? read(from + 64 * i + lane) : 0.0f;
-#pragma unroll
-        for (int i = 0; i < KEYS; ++i) held[i] = mass_key(x[i]);
-    }
-    // f(position, key) for every round of the wave
-    const auto each = [&](auto f) {
-        if constexpr (KEYS > 0) {
-            int t = from + lane;
-#pragma unroll
-            for (int i = 0; i < KEYS; ++i) {
-                asm volatile("" : "+v"(t));      // (found again every time: positions kept for all rounds would cost as many registers)
-                if (i < rounds) f(t, held[i]);
-                t += 64;
-            }
-        } else {
-            for (int i = 0; i < rounds; ++i) f(from + 64 * i + lane, mass_key(read(from + 64 * i + lane)));
+    const int upto = int(min(int64_t(r.end), a.pitch));
+    const auto each = [&](auto f) {                              // f(position, key)
+        for (int i = 0; i < rounds; ++i) {
+            const int t = from + 64 * i + lane;
+            f(t, mass_key(t < upto ? mass[t] : 0.0f));
         }
     };
     uint32_t digits = 0, mask = 0, wanted = uint32_t(max(r.wanted, 0));   // of the key that is looked for, and which are known
@@ -135,7 +247,6 @@ __global__ __launch_bounds__(SELECT_THREADS, 8) void fp4_select_kernel(Fp4Select
         const SelectBin x = find_bin(bins[2047 - 2 * tid], bins[2046 - 2 * tid], wanted, part, found);
         digits |= x.bin << shift, mask |= uint32_t(count - 1) << shift;
         wanted -= x.above;                                       // still wanted of those with these digits
-        __syncthreads();
     }
     const auto sure = [&](int t, uint32_t key) { return t < r.len && (t < r.begin || t >= r.end || (some && key > digits)); };
     const auto tie = [&](int t, uint32_t key) { return some && t >= r.begin && t < r.end && key == digits; };
@@ -143,8 +254,8 @@ __global__ __launch_bounds__(SELECT_THREADS, 8) void fp4_select_kernel(Fp4Select
     each([&](int t, uint32_t key) { sures += uint32_t(__popcll(__ballot(sure(t, key)))), ties += uint32_t(__popcll(__ballot(tie(t, key)))); });
     if (lane == 0) above[wave] = sures, equal[wave] = ties;
     __syncthreads();
-    uint32_t at = uint32_t(wave_inclusive_scan(lane < wave ? int(above[lane]) : 0)), tied = uint32_t(wave_inclusive_scan(lane < wave ? int(equal[lane]) : 0));
-    at = __builtin_amdgcn_readlane(at, 63), tied = __builtin_amdgcn_readlane(tied, 63);   // of the waves before
+    uint32_t at = 0, tied = 0;                                   // of the waves before
+    for (int i = 0; i < wave; ++i) at += above[i], tied += equal[i];
     at += min(tied, wanted);
     each([&](int t, uint32_t key) { write_kept(kept, t, sure(t, key), tie(t, key), wanted, at, tied, lane); });
 }
@@ -333,7 +444,7 @@ int launch_fp4_select(const kv_fp4_cache *c, Fp4Select a, hipStream_t s) {
     const int64_t room = int64_t(a.v.batch.table_pages) * FP4_PAGE, streams = int64_t(a.v.H) * a.v.batch.batch;
     a.parts = int((room + SELECT_PART - 1) / SELECT_PART);
     a.space = reinterpret_cast<uint32_t *>(c->workspace) + FP4_COUNTERS / sizeof(uint32_t);
-    const bool in_parts = room > 32 * SELECT_THREADS && a.parts <= SELECT_PARTS && streams * SelectSpace::words(a.parts) <= FP4_PART_ROWS * (c->cfg.head_dim + 4);
+    const bool in_parts = room > 64 * SELECT_THREADS && a.parts <= SELECT_PARTS && streams * SelectSpace::words(a.parts) <= FP4_PART_ROWS * (c->cfg.head_dim + 4);
     if (in_parts) {
         const dim3 grid = dim3(uint32_t(a.parts * a.v.H), uint32_t(a.v.batch.batch));
         hipLaunchKernelGGL(fp4_select_part_kernel<0>, grid, dim3(SELECT_THREADS), 0, s, a);
@@ -346,7 +457,8 @@ int launch_fp4_select(const kv_fp4_cache *c, Fp4Select a, hipStream_t s) {
         if (room <= 4 * SELECT_THREADS) hipLaunchKernelGGL(fp4_select_kernel<4>, grid, dim3(SELECT_THREADS), 0, s, a);
         else if (room <= 16 * SELECT_THREADS) hipLaunchKernelGGL(fp4_select_kernel<16>, grid, dim3(SELECT_THREADS), 0, s, a);
         else if (room <= 32 * SELECT_THREADS) hipLaunchKernelGGL(fp4_select_kernel<32>, grid, dim3(SELECT_THREADS), 0, s, a);
-        else hipLaunchKernelGGL(fp4_select_kernel<0>, grid, dim3(SELECT_THREADS), 0, s, a);
+        else if (room <= 64 * SELECT_THREADS) hipLaunchKernelGGL(fp4_select_kernel<64>, grid, dim3(SELECT_THREADS), 0, s, a);
+        else hipLaunchKernelGGL(fp4_select_long_kernel, grid, dim3(SELECT_THREADS), 0, s, a);
     }
     KV_HIP_CHECK(hipGetLastError());
     return KV_OK;
@@ -362,70 +474,99 @@ struct Fp4Compact {
     int64_t out_pitch;
 };
 
-// A wave to eight tokens of a kv-head where they go: a word of V's channels there takes a code from each of eight words, HD / 64
-// channels to a lane.  K's rows are 8 (4) bytes to a lane.
+// A wave to some eights of tokens of a kv-head where they go, the next eight on its way while one is written: a word of V's channels there
+// takes a code from each of eight words, HD / 64 channels to a lane; K's rows are 8 (4) bytes to a lane.  Where
+// the tokens come from -- positions, then page numbers -- is found for all of them at once, a token to a lane.
+constexpr int COMPACT_EIGHTS = 4;        // at most: 32 tokens
+constexpr int64_t COMPACT_WAVES = 8192;
 template <int HD>
-__global__ __launch_bounds__(256) void fp4_compact_kernel(Fp4Compact a, int eights) {
+struct Fp4Eight {
     using P = Fp4Block<HD>;
-    constexpr int C = HD / 64, SCALES = HD / FP4_GROUP;
-    const int lane = threadIdx.x & 63;
-    const Fp4View &v = a.from;
-    const uint32_t unit = blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int eight = int(unit / uint32_t(v.H)), h = int(unit - uint32_t(eight) * v.H), b = blockIdx.y;
-    if (eight >= eights) return;
-    const int n = min(max(a.n_kept[b], 0), a.keep), i0 = 8 * eight;
-    if (i0 >= n) return;
-    const Fp4Sequence to_seq(a.to, b, n, 0, 0);
-    const int64_t to_page = i0 / FP4_PAGE < a.to.batch.table_pages ? to_seq.page(a.to, i0 / FP4_PAGE) : -1;
-    const Fp4Sequence seq(v, b);
-    const int64_t stream = int64_t(b) * v.H + h;
-    // where each of the eight comes from, one to a lane (of eight, again and again)
-    const int j = lane & 7;
-    const int from = i0 + j < n ? a.kept[stream * a.keep + i0 + j] : -1;
-    int page = -1;
-    if (from >= 0 && from < seq.held) page = int(seq.page(v, from / FP4_PAGE));
-    if (a.mass_out && lane < 8 && i0 + j < n && i0 + j < a.out_pitch) {
-        const bool has = from >= 0 && from < a.pitch && from < seq.held;
-        a.mass_out[stream * a.out_pitch + i0 + j] = has ? a.mass[stream * a.pitch + from] : 0.0f;
-    }
-    if (to_page < 0) return;
-    uint8_t *out = v.pages + (to_page * v.H + h) * size_t(P::BYTES);
-    const int at = i0 % FP4_PAGE;
-    const uint8_t *mine = v.pages + (int64_t(max(page, 0)) * v.H + h) * size_t(P::BYTES);
-    const int slot = from & (FP4_PAGE - 1);
-    // scales: of the lane's token, group lane / 8
-    if (lane / 8 < SCALES && i0 + j < n) {
-        const int s = lane / 8;
-        out[P::KS + (at + j) * SCALES + s] = page < 0 ? uint8_t(127) : mine[P::KS + slot * SCALES + s];
-        out[P::VS + s * FP4_PAGE + at + j] = page < 0 ? uint8_t(127) : mine[P::VS + s * FP4_PAGE + slot];
-    }
-    // K: token lane / 8, an eighth of its row
-    {
-        const int t = lane / 8, part = lane & 7, p = __shfl(page, t), s = __shfl(slot, t);
-        const uint8_t *row = v.pages + (int64_t(max(p, 0)) * v.H + h) * size_t(P::BYTES) + P::K + s * (HD / 2) + part * (HD / 16);
-        uint8_t *to = out + P::K + (at + t) * (HD / 2) + part * (HD / 16);
-        if (i0 + t < n) {
-            uint32_t w[C];
+    static constexpr int C = HD / 64, SCALES = HD / FP4_GROUP;
+    uint32_t k[C], v[8][C];
+    uint8_t ks, vs;
+    // page, slot: of token (lane) of the wave's
+    __device__ inline void load(const Fp4View &view, int h, int page, int slot, int eight, int lane) {
+        const auto block = [&](int p) { return view.pages + (int64_t(max(p, 0)) * view.H + h) * size_t(P::BYTES); };
+        const int j = 8 * eight + (lane & 7), s = min(lane / 8, SCALES - 1), at = __shfl(slot, j);
+        const uint8_t *from = block(__shfl(page, j));
+        ks = from[P::KS + at * SCALES + s], vs = from[P::VS + s * FP4_PAGE + at];
+        const int t = 8 * eight + lane / 8;
+        const uint32_t *row = reinterpret_cast<const uint32_t *>(block(__shfl(page, t)) + P::K + __shfl(slot, t) * (HD / 2) + (lane & 7) * (HD / 16));
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                w[c] = p < 0 ? 0u : reinterpret_cast<const uint32_t *>(row)[c];
-                reinterpret_cast<uint32_t *>(to)[c] = w[c];
-            }
+        for (int c = 0; c < C; ++c) k[c] = row[c];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int p = __builtin_amdgcn_readlane(page, 8 * eight + i), x = __builtin_amdgcn_readlane(slot, 8 * eight + i);
+            const uint32_t *words = reinterpret_cast<const uint32_t *>(block(p) + P::V) + (x / 8) * HD + C * lane;
+#pragma unroll
+            for (int c = 0; c < C; ++c) v[i][c] = words[c];
         }
     }
-    // V: channels C * lane .. of each of the eight
-    uint32_t word[C] = {};
+    // out: the page's block; at: the first of the eight in it; n: how many there are
+    __device__ inline void store(uint8_t *out, int at, int n, int page, int slot, int eight, int lane) const {
+        const int j = lane & 7, s = lane / 8;
+        const bool there = __shfl(page, 8 * eight + j) >= 0;
+        if (s < SCALES && j < n) {
+            out[P::KS + (at + j) * SCALES + s] = there ? ks : uint8_t(127);
+            out[P::VS + s * FP4_PAGE + at + j] = there ? vs : uint8_t(127);
+        }
+        const bool row = __shfl(page, 8 * eight + s) >= 0;
+        uint32_t *to = reinterpret_cast<uint32_t *>(out + P::K + (at + s) * (HD / 2) + j * (HD / 16));
+        if (s < n) {
 #pragma unroll
-    for (int t = 0; t < 8; ++t) {
-        const int p = __builtin_amdgcn_readlane(page, t), s = __builtin_amdgcn_readlane(slot, t);
-        if (p < 0) continue;
-        const uint32_t *row = reinterpret_cast<const uint32_t *>(v.pages + (int64_t(p) * v.H + h) * size_t(P::BYTES) + P::V) + (s / 8) * HD + C * lane;
+            for (int c = 0; c < C; ++c) to[c] = row ? k[c] : 0u;
+        }
+        uint32_t word[C] = {};
 #pragma unroll
-        for (int c = 0; c < C; ++c) word[c] |= ((row[c] >> (4 * (s & 7))) & 15u) << (4 * t);
+        for (int i = 0; i < 8; ++i) {
+            const int p = __builtin_amdgcn_readlane(page, 8 * eight + i), x = __builtin_amdgcn_readlane(slot, 8 * eight + i);
+            const uint32_t keep = p >= 0 ? 15u : 0u;
+#pragma unroll
+            for (int c = 0; c < C; ++c) word[c] |= ((v[i][c] >> (4 * (x & 7))) & keep) << (4 * i);
+        }
+        uint32_t *words = reinterpret_cast<uint32_t *>(out + P::V) + (at / 8) * HD + C * lane;
+#pragma unroll
+        for (int c = 0; c < C; ++c) words[c] = word[c];
     }
-    uint32_t *to = reinterpret_cast<uint32_t *>(out + P::V) + (at / 8) * HD + C * lane;
-#pragma unroll
-    for (int c = 0; c < C; ++c) to[c] = word[c];
+};
+
+template <int HD>
+__global__ __launch_bounds__(256) void fp4_compact_kernel(Fp4Compact a, int units, int eights_of_wave) {
+    using P = Fp4Block<HD>;
+    const int lane = threadIdx.x & 63;
+    const Fp4View &v = a.from;
+    const uint32_t number = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int unit = int(number / uint32_t(v.H)), h = int(number - uint32_t(unit) * v.H), b = blockIdx.y;
+    if (unit >= units) return;
+    const int n = min(max(a.n_kept[b], 0), a.keep);
+    const int64_t first = int64_t(unit) * 8 * eights_of_wave;
+    if (first >= n) return;
+    const int i0 = int(first), here = min(n - i0, 8 * eights_of_wave), eights = (here + 7) / 8;
+    const Fp4Sequence to_seq(a.to, b, n, 0, 0), seq(v, b);
+    const int64_t stream = int64_t(b) * v.H + h;
+    // token `lane` of the wave's: where it comes from, and the page that it goes to
+    const int from = lane < here ? a.kept[stream * a.keep + i0 + lane] : -1;
+    const bool held = from >= 0 && from < seq.held;
+    const int page = held ? int(seq.page(v, from / FP4_PAGE)) : -1, slot = from & (FP4_PAGE - 1);
+    const int to_page = lane < here && (i0 + lane) / FP4_PAGE < a.to.batch.table_pages ? int(to_seq.page(a.to, (i0 + lane) / FP4_PAGE)) : -1;
+    if (a.mass_out && lane < here && i0 + lane < a.out_pitch)
+        a.mass_out[stream * a.out_pitch + i0 + lane] = held && from < a.pitch ? a.mass[stream * a.pitch + from] : 0.0f;
+    const auto store = [&](const Fp4Eight<HD> &x, int e) {
+        const int to = __builtin_amdgcn_readlane(to_page, 8 * e);
+        if (to < 0) return;
+        x.store(v.pages + (int64_t(to) * v.H + h) * size_t(P::BYTES), (i0 + 8 * e) % FP4_PAGE, min(here - 8 * e, 8), page, slot, e, lane);
+    };
+    Fp4Eight<HD> in[2];
+    in[0].load(v, h, page, slot, 0, lane);
+    for (int e = 0;; e += 2) {           // (behind the last eight that one again)
+        in[1].load(v, h, page, slot, min(e + 1, eights - 1), lane);
+        store(in[0], e);
+        if (e + 1 >= eights) break;
+        in[0].load(v, h, page, slot, min(e + 2, eights - 1), lane);
+        store(in[1], e + 1);
+        if (e + 2 >= eights) break;
+    }
 }
 
 }  // namespace packkv
@@ -452,12 +593,14 @@ extern "C" int kv_fp4_compact(kv_fp4_cache_t *c, const kv_fp4_batch_t *from, con
     if (!mass != !mass_out) return KV_ERR_ARG;
     if (mass && (mass_tokens < 1 || mass_out_tokens < 1 || !fp4_aligned(mass, 4) || !fp4_aligned(mass_out, 4))) return KV_ERR_ARG;
     const Fp4Compact a{fp4_view(c, from, 0), fp4_view(c, to, 0), kept, n_kept, keep, mass, mass_tokens, mass_out, mass_out_tokens};
-    const int64_t eights = (int64_t(keep) + 7) / 8, groups = (eights * c->cfg.n_kv_heads + 3) / 4;
+    // several eights to a wave where there are more waves than run at once
+    const int64_t eights = (int64_t(keep) + 7) / 8, each = eights * c->cfg.n_kv_heads * from->batch >= COMPACT_WAVES ? COMPACT_EIGHTS : 1;
+    const int64_t units = (eights + each - 1) / each, groups = (units * c->cfg.n_kv_heads + 3) / 4;
     if (groups > FP4_GROUPS_MOST) return KV_ERR_UNSUPPORTED;
     const dim3 grid = dim3(uint32_t(groups), uint32_t(from->batch));
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    if (c->cfg.head_dim == 128) hipLaunchKernelGGL(fp4_compact_kernel<128>, grid, dim3(256), 0, s, a, int(eights));
-    else hipLaunchKernelGGL(fp4_compact_kernel<64>, grid, dim3(256), 0, s, a, int(eights));
+    if (c->cfg.head_dim == 128) hipLaunchKernelGGL(fp4_compact_kernel<128>, grid, dim3(256), 0, s, a, int(units), int(each));
+    else hipLaunchKernelGGL(fp4_compact_kernel<64>, grid, dim3(256), 0, s, a, int(units), int(each));
     KV_HIP_CHECK(hipGetLastError());
     return KV_OK;
 }
