@@ -35,7 +35,8 @@ __device__ constexpr int select_bins(int pass) { return pass == 2 ? 1024 : 2048;
 struct SelectRange {
     int len, budget, n, begin, end, wanted;   // wanted: of the tokens begin .. end - 1, whose weights decide
     __device__ inline SelectRange(const Fp4Select &a, const Fp4Sequence &seq, int b) {
-        len = seq.held, budget = min(a.budgets ? max(a.budgets[b], 0) : a.keep, a.keep), n = min(len, budget);
+        len = __builtin_amdgcn_readfirstlane(seq.held);
+        budget = __builtin_amdgcn_readfirstlane(min(a.budgets ? max(a.budgets[b], 0) : a.keep, a.keep)), n = min(len, budget);
         const int sinks = min(a.sinks, budget), recent = min(a.recent, budget - sinks);
         begin = sinks, end = len - recent, wanted = budget - sinks - recent;
     }
@@ -81,29 +82,19 @@ __device__ inline void write_kept(int32_t *kept, int t, bool sure, bool tie, uin
     at += uint32_t(__popcll(keeps)), tied += uint32_t(__popcll(ties));
 }
 
-// The threads' numbers of something, up to this thread's (excluded), and of all.  All threads call; sums: LDS.  Contains a barrier.
-__device__ inline uint32_t sum_before(uint32_t mine, uint32_t *sums, uint32_t *all) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t upto = uint32_t(wave_inclusive_scan(int(mine)));
-    if (lane == 63) sums[wave] = upto;
-    __syncthreads();
-    const uint32_t waves = uint32_t(wave_inclusive_scan(lane < SELECT_WAVES ? int(sums[lane]) : 0));
-    *all = __builtin_amdgcn_readlane(waves, 63);
-    return upto - mine + (wave ? __builtin_amdgcn_readlane(waves, (__builtin_amdgcn_readfirstlane(wave) - 1) & 63) : 0u);
-}
-
-// A workgroup to a (sequence, kv-head), up to KEYS tokens in a row to a thread, whose keys are read once and stay in registers: which of them
-// are kept is bits of a word, positions come from one sum over the threads.  The keys with the first digit that is found go to LDS
-// and the others are found among them, if there is room.  Bound by vector instructions (some 30 to a token and lane) and LDS.
-constexpr uint32_t KEY_OF_0 = 0x80000000u, KEY_OF_NONE = 0;      // (no number has the key 0)
+// A workgroup to a (sequence, kv-head), a wave to a sixteenth of the tokens, four in a row to a lane, 256 at a time.  Up to KEYS
+// keys of a lane are read once and stay in registers; which of them are kept is bits of a word.  The first digit's counting takes
+// no branches: what does not count is counted in a place of the lane's own.
+constexpr uint32_t KEY_OF_0 = 0x80000000u, KEY_OF_NONE = 0;      // (no number has the key 0, or one of its first digit)
 constexpr int SELECT_LIST = 4096;
 template <int KEYS>
-__global__ __launch_bounds__(SELECT_THREADS, KEYS > 32 ? 4 : 8) void fp4_select_kernel(Fp4Select a) {
+__global__ __launch_bounds__(SELECT_THREADS, 4) void fp4_select_kernel(Fp4Select a) {
     using Bits = std::conditional_t<(KEYS > 32), uint64_t, uint32_t>;
-    __shared__ uint32_t bins[SELECT_BINS], list[SELECT_LIST];
-    __shared__ uint32_t found[2], part[SELECT_WAVES], sums[2][SELECT_WAVES];
+    constexpr int CHUNKS = KEYS / 4;
+    __shared__ uint32_t bins[SELECT_BINS + 64], list[SELECT_LIST];
+    __shared__ uint32_t found[2], part[SELECT_WAVES], sums[2][SELECT_WAVES], listed;
     const Fp4View &v = a.v;
-    const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+    const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Fp4Sequence seq(v, b);
     const SelectRange r(a, seq, b);
     const int64_t stream = int64_t(b) * v.H + h;
@@ -115,99 +106,148 @@ __global__ __launch_bounds__(SELECT_THREADS, KEYS > 32 ? 4 : 8) void fp4_select_
         for (int i = tid; i < r.n; i += SELECT_THREADS) kept[i] = i;
         return;
     }
-    // this thread's tokens, a multiple of four
-    const int mine = ((r.len + SELECT_THREADS - 1) / SELECT_THREADS + 3) & ~3, t0 = tid * mine;
+    const int chunks = (r.len + 256 * SELECT_WAVES - 1) / (256 * SELECT_WAVES), from = 256 * chunks * wave, t0 = from + 4 * lane;
     const int upto = int(min(int64_t(r.len), a.pitch));          // (tokens without a place have weight 0)
-    const auto below = [&](int t) {                              // bits of the tokens below position t
-        const int n = min(max(t - t0, 0), mine);
-        return n < int(8 * sizeof(Bits)) ? (Bits(1) << n) - 1 : ~Bits(0);
-    };
-    const Bits decides = r.wanted > 0 ? below(r.end) & ~below(r.begin) : 0;
-    uint32_t key[KEYS];
     typedef float four_t __attribute__((ext_vector_type(4), aligned(4)));
+    const float *base = upto < 4 ? reinterpret_cast<const float *>(v.pages) : mass;
+    const int last = max(upto - 4, 0);
+    uint32_t key[KEYS];
 #pragma unroll
-    for (int i = 0; i < KEYS; i += 4) {
-        float x[4] = {0, 0, 0, 0};
-        if (i < mine) {
-            if (t0 + i + 4 <= upto) {
-                const four_t y = *reinterpret_cast<const four_t *>(mass + t0 + i);
-                x[0] = y[0], x[1] = y[1], x[2] = y[2], x[3] = y[3];
-            } else {
+    for (int i = 0; i < CHUNKS; ++i) {
+        // (the last four there are where there would be fewer; behind the last chunk some again, which do not decide)
+        const int t = t0 + 256 * min(i, chunks - 1);
+        const uint32_t at = 4u * uint32_t(min(t, last));
+        const four_t x = *reinterpret_cast<const four_t *>(reinterpret_cast<const char *>(base) + at);
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (t0 + i + j < upto) x[j] = mass[t0 + i + j];
+        for (int j = 0; j < 4; ++j) key[4 * i + j] = __float_as_uint(x[j]);
+        if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+    }
+    if (from + 256 * chunks > upto) {                            // (wave-uniform)
+#pragma unroll
+        for (int i = 0; i < CHUNKS; ++i) {
+            const int t = t0 + 256 * i, past = t + 4 - upto;     // the four are `past` places too early
+            uint32_t *x = key + 4 * i;
+            if (past > 0) {
+                x[0] = past == 1 ? x[1] : past == 2 ? x[2] : past == 3 ? x[3] : 0u;
+                x[1] = past == 1 ? x[2] : past == 2 ? x[3] : 0u;
+                x[2] = past == 1 ? x[3] : 0u;
+                x[3] = 0u;
+            }
+            if (i == 0 && t == 0 && upto < 4) {
+#pragma unroll
+                for (int j = 0; j < 3; ++j) x[j] = j < upto ? __float_as_uint(mass[min(j, upto - 1)]) : 0u;
             }
         }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) key[i + j] = __float_as_uint(x[j]);
     }
+    // Weights are hardly ever negative or NaN: a key is then the number's bits with the highest set.
+    uint32_t largest = 0;
 #pragma unroll
-    for (int i = 0; i < KEYS; ++i) key[i] = (decides >> i) & 1 ? mass_key(__uint_as_float(key[i])) : KEY_OF_NONE;
+    for (int i = 0; i < KEYS; ++i) largest = max(largest, key[i]);
+    if (__any(largest > 0x7F800000u)) {
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) key[i] = mass_key(__uint_as_float(key[i]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) key[i] |= KEY_OF_0;
+    }
+    // Bits of the tokens that there are, and of those that decide; others have no key.
+    Bits there = 4 * chunks < int(8 * sizeof(Bits)) ? (Bits(1) << (4 * chunks)) - 1 : ~Bits(0), decides = there;
+    if (from < r.begin || from + 256 * chunks > r.end) {           // (wave-uniform)
+        there = decides = 0;
+        for (int i = 0; i < chunks; ++i) {
+            const auto below = [&](int t) { return (1u << min(max(t - (t0 + 256 * i), 0), 4)) - 1; };
+            there |= Bits(below(r.len)) << (4 * i), decides |= Bits(below(r.end) & ~below(r.begin)) << (4 * i);
+        }
+    }
+    if (decides != ~Bits(0)) {
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) key[i] = (decides >> i) & 1 ? key[i] : KEY_OF_NONE;
+    }
 
-    Bits sure = below(r.begin) | (below(r.len) & ~below(r.end)), tie = 0;
+    Bits sure = there & ~decides, tie = 0;
     uint32_t wanted = uint32_t(max(r.wanted, 0));
     if (wanted > 0) {                                            // (uniform)
-        for (int i = tid; i < SELECT_BINS; i += SELECT_THREADS) bins[i] = 0;
-        __syncthreads();
+        const auto clear = [&]() {
+            bins[tid] = bins[tid + SELECT_THREADS] = 0;
+            __syncthreads();
+        };
+        if (tid == 0) listed = 0;
+        clear();
         // weights of 0 are many where a window hides tokens: counted for the wave
         uint32_t zeros = 0;
 #pragma unroll
         for (int i = 0; i < KEYS; ++i) {
-            if (i < mine) {
-                zeros += uint32_t(__popcll(__ballot(key[i] == KEY_OF_0)));
-                if (key[i] << 1) atomicAdd(&bins[key[i] >> select_shift(0)], 1u);
-            }
+            if (i >= 4 * chunks) continue;
+            zeros += uint32_t(__popcll(__ballot(key[i] == KEY_OF_0)));
+            atomicAdd(&bins[key[i] << 1 ? key[i] >> select_shift(0) : SELECT_BINS + lane], 1u);
+            if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (else places of all keys are found first, in as many registers)
         }
         if (lane == 0 && zeros) atomicAdd(&bins[KEY_OF_0 >> select_shift(0)], zeros);
         __syncthreads();
         SelectBin x = find_bin(bins[2047 - 2 * tid], bins[2046 - 2 * tid], wanted, part, found);
         wanted -= x.above;
         uint32_t digits = x.bin << select_shift(0), mask = 0xFFFFFFFFu << select_shift(0);
-        Bits in = 0;
-        uint32_t total;
+        // The keys with the digit, in any order, in LDS if there is room.
+        const uint32_t total = bins[x.bin];
+        const bool room = total <= SELECT_LIST;
+        if (room) {
+            Bits in = 0;
 #pragma unroll
-        for (int i = 0; i < KEYS; ++i) in |= Bits(key[i] >> select_shift(0) == x.bin) << i;
-        in &= decides;
-        uint32_t at = sum_before(uint32_t(__popcll(uint64_t(in))), sums[0], &total);
-        const bool listed = total <= SELECT_LIST;
-        if (listed) {
+            for (int i = 0; i < KEYS; ++i) in |= Bits(key[i] - digits < 1u << select_shift(0)) << i;
+            const uint32_t own = uint32_t(__popcll(uint64_t(in))), to = uint32_t(wave_inclusive_scan(int(own)));
+            uint32_t at = 0;
+            if (lane == 63 && to) at = atomicAdd(&listed, to);
+            at = uint32_t(__builtin_amdgcn_readlane(int(at), 63)) + to - own;
 #pragma unroll
             for (int i = 0; i < KEYS; ++i)
                 if ((in >> i) & 1) list[at++] = key[i];
         }
         for (int pass = 1; pass < 3; ++pass) {
             const int shift = select_shift(pass), count = select_bins(pass);
-            for (int i = tid; i < SELECT_BINS; i += SELECT_THREADS) bins[i] = 0;
-            __syncthreads();
-            if (listed) {
-                for (uint32_t j = tid - lane; j < total; j += SELECT_THREADS) {
+            __syncthreads();                                     // (all have read bins)
+            clear();
+            if (room) {
+                for (uint32_t j = 64 * wave; j < total; j += SELECT_THREADS) {
                     const uint32_t k = j + lane < total ? list[j + lane] : 0u;
                     count_key(bins, (k >> shift) & (count - 1), j + lane < total && ((k ^ digits) & mask) == 0);
                 }
-            } else {
-#pragma unroll
-                for (int i = 0; i < KEYS; ++i)
-                    if (i < mine) count_key(bins, (key[i] >> shift) & (count - 1), key[i] != KEY_OF_NONE && ((key[i] ^ digits) & mask) == 0);
+            } else {                                             // (read again: seldom)
+                for (int i = 0; i < 4 * chunks; ++i) {
+                    const int t = from + 64 * i + lane;
+                    const uint32_t k = mass_key(t < upto ? mass[t] : 0.0f);
+                    count_key(bins, (k >> shift) & (count - 1), t >= r.begin && t < r.end && ((k ^ digits) & mask) == 0);
+                }
             }
             __syncthreads();
             x = find_bin(bins[2047 - 2 * tid], bins[2046 - 2 * tid], wanted, part, found);
             digits |= x.bin << shift, mask |= uint32_t(count - 1) << shift;
             wanted -= x.above;
         }
+        if (bins[x.bin] == wanted) {                             // all of the tied ones
 #pragma unroll
-        for (int i = 0; i < KEYS; ++i) sure |= Bits(key[i] > digits) << i, tie |= Bits(key[i] == digits) << i;
+            for (int i = 0; i < KEYS; ++i) sure |= Bits(key[i] >= digits) << i;
+        } else {
+#pragma unroll
+            for (int i = 0; i < KEYS; ++i) sure |= Bits(key[i] > digits) << i, tie |= Bits(key[i] == digits) << i;
+        }
     }
-    // of the tied ones as many as are still wanted, from the front
-    uint32_t all;
-    const uint32_t before = sum_before(uint32_t(__popcll(uint64_t(tie))), sums[1], &all);
-    for (uint32_t n = before < wanted ? wanted - before : 0; n && tie; --n) {
-        sure |= tie & (~tie + 1);
-        tie &= tie - 1;
-    }
-    uint32_t at = sum_before(uint32_t(__popcll(uint64_t(sure))), sums[0], &all);
-    while (sure) {
-        kept[at++] = t0 + __builtin_ctzll(uint64_t(sure));
-        sure &= sure - 1;
+    const auto wave_sum = [](uint32_t n) { return uint32_t(__builtin_amdgcn_readlane(wave_inclusive_scan(int(n)), 63)); };
+    const uint32_t mine[2] = {wave_sum(uint32_t(__popcll(uint64_t(sure)))), wave_sum(uint32_t(__popcll(uint64_t(tie))))};
+    if (lane == 0) sums[0][wave] = mine[0], sums[1][wave] = mine[1];
+    __syncthreads();
+    uint32_t tied = wave_sum(lane < wave ? sums[1][lane] : 0u);  // in the waves before
+    uint32_t at = wave_sum(lane < wave ? sums[0][lane] : 0u) + min(tied, wanted);
+    for (int i = 0; i < chunks; ++i) {
+        uint32_t keep = uint32_t(sure >> (4 * i)) & 15u, more = uint32_t(tie >> (4 * i)) & 15u;
+        if (mine[1]) {       // (wave-uniform) of the tied ones as many as are still wanted, from the front
+            const uint32_t own = __popc(more), to = uint32_t(wave_inclusive_scan(int(own))), before = tied + to - own;
+            for (uint32_t n = before < wanted ? wanted - before : 0u; n && more; --n) keep |= more & (~more + 1), more &= more - 1;
+            tied += __builtin_amdgcn_readlane(to, 63);
+        }
+        const uint32_t own = __popc(keep), to = uint32_t(wave_inclusive_scan(int(own)));
+        uint32_t place = at + to - own;
+        for (; keep; keep &= keep - 1) kept[place++] = t0 + 256 * i + __builtin_ctz(keep);
+        at += __builtin_amdgcn_readlane(to, 63);
     }
 }
 
@@ -444,7 +484,7 @@ int launch_fp4_select(const kv_fp4_cache *c, Fp4Select a, hipStream_t s) {
     const int64_t room = int64_t(a.v.batch.table_pages) * FP4_PAGE, streams = int64_t(a.v.H) * a.v.batch.batch;
     a.parts = int((room + SELECT_PART - 1) / SELECT_PART);
     a.space = reinterpret_cast<uint32_t *>(c->workspace) + FP4_COUNTERS / sizeof(uint32_t);
-    const bool in_parts = room > 64 * SELECT_THREADS && a.parts <= SELECT_PARTS && streams * SelectSpace::words(a.parts) <= FP4_PART_ROWS * (c->cfg.head_dim + 4);
+    const bool in_parts = room > 40 * SELECT_THREADS && a.parts <= SELECT_PARTS && streams * SelectSpace::words(a.parts) <= FP4_PART_ROWS * (c->cfg.head_dim + 4);
     if (in_parts) {
         const dim3 grid = dim3(uint32_t(a.parts * a.v.H), uint32_t(a.v.batch.batch));
         hipLaunchKernelGGL(fp4_select_part_kernel<0>, grid, dim3(SELECT_THREADS), 0, s, a);
@@ -457,7 +497,7 @@ int launch_fp4_select(const kv_fp4_cache *c, Fp4Select a, hipStream_t s) {
         if (room <= 4 * SELECT_THREADS) hipLaunchKernelGGL(fp4_select_kernel<4>, grid, dim3(SELECT_THREADS), 0, s, a);
         else if (room <= 16 * SELECT_THREADS) hipLaunchKernelGGL(fp4_select_kernel<16>, grid, dim3(SELECT_THREADS), 0, s, a);
         else if (room <= 32 * SELECT_THREADS) hipLaunchKernelGGL(fp4_select_kernel<32>, grid, dim3(SELECT_THREADS), 0, s, a);
-        else if (room <= 64 * SELECT_THREADS) hipLaunchKernelGGL(fp4_select_kernel<64>, grid, dim3(SELECT_THREADS), 0, s, a);
+        else if (room <= 40 * SELECT_THREADS) hipLaunchKernelGGL(fp4_select_kernel<40>, grid, dim3(SELECT_THREADS), 0, s, a);
         else hipLaunchKernelGGL(fp4_select_long_kernel, grid, dim3(SELECT_THREADS), 0, s, a);
     }
     KV_HIP_CHECK(hipGetLastError());
