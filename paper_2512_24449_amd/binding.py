@@ -89,7 +89,7 @@ EXPORTS = ("kv_query_sizes", "kv_cache_create", "kv_cache_destroy", "kv_compress
 # entry points the native module calls, in its order
 _NATIVE_CALLS = ("kv_compress_append", "kv_compress_append_bf16", "kv_k_matvec", "kv_softmax", "kv_v_matvec",
                  "kv_decode_attention", "kv_cache_restore", "kv_cache_release", "kv_cache_tokens", "kv_fp4_append", "kv_fp4_read",
-                 "kv_fp4_attention")
+                 "kv_fp4_attention", "kv_fp4_weights", "kv_fp4_select", "kv_fp4_compact", "kv_rotary")
 
 _lib = None
 _native = None
@@ -126,6 +126,7 @@ class _PythonCalls:
         return NotImplemented
 
     k_matvec = softmax = v_matvec = attention = restore = release = read = append
+    read_into = weights = select = compact = turn = append
 
 
 def lib():
@@ -623,6 +624,10 @@ class FP4KVCache(_Operators):
             done = self._calls.read(batch._address, batch._on, n_rows, dtype, stream)
             if done is not NotImplemented:
                 return done
+        elif k is not None and v is not None and k.dtype == dtype:
+            done = self._calls.read_into(batch._address, batch._on, n_rows, k, v, stream)
+            if done is not NotImplemented:
+                return done
         what, shape = "kv_fp4_read", (n_rows, self.n_kv_heads, self.head_dim)
         if dtype not in _TYPES:
             _refuse(what, "dtype is float16, bfloat16 or float32")
@@ -664,6 +669,10 @@ class FP4KVCache(_Operators):
         q, sm_scale, window and sinks as kv_fp4_attention had them, lse as it gave them; past: null, or of out's shape, or out
         itself; it counts for the tokens before the new rows.  Without out a new tensor of past's shape, or of the page table's
         width, zeros where the sequences have no tokens; places of out behind a sequence's tokens are not written."""
+        if out is not None:
+            done = self._calls.weights(q, lse, batch._address, batch._on, sm_scale, window, sinks, past, out, stream)
+            if done is not NotImplemented:
+                return done
         what, tokens = "kv_fp4_weights", 64 * batch.table_pages
         rows, q_stride = self._rows(what, q, self.n_q_heads, (torch.float16, torch.bfloat16))
         on = self._stream(stream)
@@ -688,6 +697,10 @@ class FP4KVCache(_Operators):
         """Which tokens the batch's sequences keep, of mass [batch, H_kv, tokens] (kv_fp4_weights): (kept, n_kept), int32 [batch, H_kv,
         keep], positions in ascending order and -1 behind them, and int32 [batch].  All of a sequence of no more than keep (or
         budgets[b], int32 [batch]) tokens; else the first `sinks`, the last `recent` and the others of the largest mass."""
+        if budgets is None and kept is None:
+            done = self._calls.select(mass, batch._address, batch._on, keep, sinks, recent, n_kept, stream)
+            if done is not NotImplemented:
+                return done
         what = "kv_fp4_select"
         keep = int(keep)
         if mass.dim() != 3 or not (1 <= keep < 2 ** 31 and 0 <= sinks < 2 ** 31 and 0 <= recent < 2 ** 31):
@@ -708,6 +721,9 @@ class FP4KVCache(_Operators):
         the pages of `to`, an FP4Batch of as many sequences whose pages the call does not read (its lens may be n_kept).  mass: weights
         that go with them, [batch, H_kv, tokens], into mass_out, [batch, H_kv, any number] (without it new, [batch, H_kv, keep], zeros
         behind the kept ones), which is returned."""
+        done = self._calls.compact(kept, n_kept, batch._address, batch._on, to._address, to._on, mass, mass_out, stream)
+        if done is not NotImplemented:
+            return done
         what, keep = "kv_fp4_compact", kept.shape[-1]
         shape, on = (batch.batch, self.n_kv_heads, keep), self._stream(stream)
         kept_at = self._plain(what, "kept", kept, torch.int32, shape)
@@ -761,6 +777,7 @@ class Rotary(_Operators):
         self.device = self._turns.device
         self._c = kv_rotary_t(head_dim, dims, int(self.interleaved), magnitude, self._turns.data_ptr())
         self._ref = C.byref(self._c)
+        self._calls = _native.RotaryCalls(C.addressof(self._c), head_dim, str(self.device)) if _native else _PythonCalls()
 
     @staticmethod
     def _frequencies(what, dims, base, scaling, factor, original, low, high, slow, fast):
@@ -793,6 +810,9 @@ class Rotary(_Operators):
         """q, k: fp16, bf16 or fp32 [rows, heads, head_dim] (or [batch, n, heads, head_dim]), both of one type; may be parts of wider rows.
         positions: int32, of q's shape without the last two axes.  Returns what became of q, or of (q, k); out and k_out: where to, which
         may be q and k themselves.  inverse: turned the other way."""
+        done = self._calls.turn(q, positions, k, out, k_out, inverse, stream)
+        if done is not NotImplemented:
+            return done
         what, types = "kv_rotary", (torch.float16, torch.bfloat16, torch.float32)
         on, args, kept = self._stream(stream), [], [positions]
         if positions.dtype != torch.int32 or positions.device != self.device or not positions.is_contiguous() or \

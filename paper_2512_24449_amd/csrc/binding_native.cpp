@@ -1,4 +1,4 @@
-// The calls of a decode step and of an append, marshalled in C++: binding.PackedKVCache and binding.FP4KVCache try these first.  A call whose
+// The calls of a decode step and of an append, marshalled in C++: binding.PackedKVCache, binding.FP4KVCache and binding.Rotary try these first.  A call whose
 // arguments are not exactly what it expects (plain tensors of the right type, shape and layout) is answered with
 // NotImplemented and made again by the Python code, which has the checks and raises the errors.
 //
@@ -15,6 +15,8 @@
 #include <cstdint>
 #include <cstring>
 #include <string>
+
+#include "../../include/packkv.h"
 
 namespace {
 
@@ -33,6 +35,14 @@ struct Library {
     int (*fp4_read)(void *, const void *, void *, void *, int32_t, int64_t, void *);
     int (*fp4_attention)(void *, const void *, const void *, int64_t, int32_t, int64_t, float, int32_t, int32_t, void *, int32_t,
                          float *, void *);
+    int (*fp4_weights)(void *, const void *, const void *, int64_t, int32_t, int64_t, float, int32_t, int32_t, const float *,
+                       const float *, float *, int64_t, void *);
+    int (*fp4_select)(void *, const void *, const float *, int64_t, int32_t, const int32_t *, int32_t, int32_t, int32_t *, int32_t *,
+                      void *);
+    int (*fp4_compact)(void *, const void *, const void *, const int32_t *, int32_t, const int32_t *, const float *, int64_t, float *,
+                       int64_t, void *);
+    int (*rotary)(const void *, const int32_t *, int64_t, int32_t, int32_t, const void *, int64_t, int32_t, void *, int64_t, const void *,
+                  int64_t, int32_t, void *, int64_t, void *);
 } lib;
 PyObject *check_code, *get_device, *get_stream, *in_bad_fork;
 
@@ -233,13 +243,13 @@ struct FP4Calls {
     c10::Device device;
 };
 
-// torch's current stream, if the cache's device is the current one.
-bool current_stream(const FP4Calls *c, void *&out) {
+// torch's current stream, if `on` is the current device.
+bool current_stream(const c10::Device &on, void *&out) {
     PyObject *bad = PyObject_CallNoArgs(in_bad_fork);
     const bool fine = bad == Py_False;
     Py_XDECREF(bad);
     PyObject *device = fine ? PyObject_CallNoArgs(get_device) : nullptr;
-    PyObject *raw = device && PyLong_AsLong(device) == c->device.index() ? PyObject_CallOneArg(get_stream, device) : nullptr;
+    PyObject *raw = device && PyLong_AsLong(device) == on.index() ? PyObject_CallOneArg(get_stream, device) : nullptr;
     Py_XDECREF(device);
     if (raw) out = PyLong_AsVoidPtr(raw);
     Py_XDECREF(raw);
@@ -289,7 +299,7 @@ PyObject *fp4_append(FP4Calls *c, PyObject *const *args, Py_ssize_t n) {   // k,
     Rows k, v;
     if (n != 5 || !c->handle || args[4] != Py_None || modes() || !batch_of(c, args[2], args[3], batch) ||
         !rows_of(c, args[0], c->kv_heads, k) || !rows_of(c, args[1], c->kv_heads, v) || k.rows != v.rows ||
-        k.t->scalar_type() != v.t->scalar_type() || !current_stream(c, s))
+        k.t->scalar_type() != v.t->scalar_type() || !current_stream(c->device, s))
         return slow();
     const void *kp = k.t->data_ptr(), *vp = v.t->data_ptr();
     const int32_t type = type_of(k.t->scalar_type());
@@ -307,7 +317,7 @@ PyObject *fp4_read(FP4Calls *c, PyObject *const *args, Py_ssize_t n) {   // batc
         !THPDtype_Check(args[3]))
         return slow();
     const c10::ScalarType type = reinterpret_cast<THPDtype *>(args[3])->scalar_type;
-    if ((type != at::kHalf && type != at::kBFloat16 && type != at::kFloat) || !current_stream(c, s)) return slow();
+    if ((type != at::kHalf && type != at::kBFloat16 && type != at::kFloat) || !current_stream(c->device, s)) return slow();
     const at::TensorOptions options = at::TensorOptions().dtype(type).device(c->device);
     const at::Tensor k = at::empty({rows, c->kv_heads, c->head_dim}, options), v = at::empty({rows, c->kv_heads, c->head_dim}, options);
     void *kp = k.data_ptr(), *vp = v.data_ptr();
@@ -328,7 +338,7 @@ PyObject *fp4_attention(FP4Calls *c, PyObject *const *args, Py_ssize_t n) {   //
     int32_t window, sinks;
     Rows q;
     if (n != 7 || !c->handle || args[6] != Py_None || modes() || !batch_of(c, args[1], args[2], batch) || !scale_of(args[3], scale) ||
-        !count_of(args[4], window) || !count_of(args[5], sinks) || !rows_of(c, args[0], c->q_heads, q) || !current_stream(c, s))
+        !count_of(args[4], window) || !count_of(args[5], sinks) || !rows_of(c, args[0], c->q_heads, q) || !current_stream(c->device, s))
         return slow();
     const c10::ScalarType type = q.t->scalar_type();
     const at::Tensor out = at::empty({q.rows, c->q_heads, c->head_dim}, at::TensorOptions().dtype(type).device(c->device));
@@ -337,6 +347,199 @@ PyObject *fp4_attention(FP4Calls *c, PyObject *const *args, Py_ssize_t n) {   //
     const int32_t t = type_of(type);
     const int code = unlocked([&] { return lib.fp4_attention(c->handle, batch, qp, q.pitch, t, q.rows, scale, window, sinks, op, t, nullptr, s); });
     return answer(code, "kv_fp4_attention", THPVariable_Wrap(out));
+    END_HANDLE_TH_ERRORS
+}
+
+// A contiguous tensor of `type` on the device; its shape is the caller's to look at.
+const at::Tensor *plain_on(const c10::Device &device, PyObject *o, c10::ScalarType type) {
+    if (!plain(o, type)) return nullptr;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    return t.device() == device && !t.is_neg() ? &t : nullptr;
+}
+
+int32_t sequences(const void *batch) { return static_cast<const kv_fp4_batch_t *>(batch)->batch; }
+
+bool streams_of(const FP4Calls *c, const at::Tensor &t, const void *batch) {
+    return t.dim() == 3 && t.size(0) == sequences(batch) && t.size(1) == c->kv_heads;
+}
+
+PyObject *fp4_read_into(FP4Calls *c, PyObject *const *args, Py_ssize_t n) {   // batch, its device, n_rows, k, v, stream
+    HANDLE_TH_ERRORS
+    void *s;
+    const void *batch;
+    int32_t rows;
+    if (n != 6 || !c->handle || args[5] != Py_None || modes() || !batch_of(c, args[0], args[1], batch) || !count_of(args[2], rows) ||
+        !THPVariable_CheckExact(args[3]))
+        return slow();
+    const c10::ScalarType type = THPVariable_Unpack(args[3]).scalar_type();
+    if (type != at::kHalf && type != at::kBFloat16 && type != at::kFloat) return slow();
+    const at::Tensor *k = plain_on(c->device, args[3], type), *v = plain_on(c->device, args[4], type);
+    for (const at::Tensor *t : {k, v})
+        if (!t || t->dim() != 3 || t->size(0) != rows || t->size(1) != c->kv_heads || t->size(2) != c->head_dim) return slow();
+    if (!current_stream(c->device, s)) return slow();
+    void *kp = k->data_ptr(), *vp = v->data_ptr();
+    const int code = unlocked([&] { return lib.fp4_read(c->handle, batch, kp, vp, type_of(type), rows, s); });
+    return answer(code, "kv_fp4_read", PyTuple_Pack(2, args[3], args[4]));
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject *fp4_weights(FP4Calls *c, PyObject *const *args, Py_ssize_t n) {   // q, lse, batch, its device, sm_scale, window, sinks, past, out, stream
+    HANDLE_TH_ERRORS
+    void *s;
+    const void *batch;
+    float scale;
+    int32_t window, sinks;
+    Rows q;
+    if (n != 10 || !c->handle || args[9] != Py_None || modes() || !batch_of(c, args[2], args[3], batch) || !scale_of(args[4], scale) ||
+        !count_of(args[5], window) || !count_of(args[6], sinks) || !rows_of(c, args[0], c->q_heads, q))
+        return slow();
+    const at::Tensor *lse = plain_on(c->device, args[1], at::kFloat), *out = plain_on(c->device, args[8], at::kFloat);
+    const bool added = args[7] != Py_None;
+    const at::Tensor *past = added ? plain_on(c->device, args[7], at::kFloat) : nullptr;
+    if (!lse || lse->dim() != 2 || lse->size(0) != q.rows || lse->size(1) != c->q_heads || !out || !streams_of(c, *out, batch) ||
+        (added && (!past || past->sizes() != out->sizes())) || !current_stream(c->device, s))
+        return slow();
+    const void *qp = q.t->data_ptr();
+    const float *lp = static_cast<const float *>(lse->data_ptr()), *pp = added ? static_cast<const float *>(past->data_ptr()) : nullptr;
+    float *op = static_cast<float *>(out->data_ptr());
+    const int32_t type = type_of(q.t->scalar_type());
+    const int64_t tokens = out->size(2);
+    const int code = unlocked([&] {
+        return lib.fp4_weights(c->handle, batch, qp, q.pitch, type, q.rows, scale, window, sinks, lp, pp, op, tokens, s);
+    });
+    return answer(code, "kv_fp4_weights", Py_NewRef(args[8]));
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject *fp4_select(FP4Calls *c, PyObject *const *args, Py_ssize_t n) {   // mass, batch, its device, keep, sinks, recent, n_kept, stream; kept is new
+    HANDLE_TH_ERRORS
+    void *s;
+    const void *batch;
+    int32_t keep, sinks, recent;
+    if (n != 8 || !c->handle || args[7] != Py_None || modes() || !batch_of(c, args[1], args[2], batch) || !count_of(args[3], keep) || keep < 1 ||
+        !count_of(args[4], sinks) || !count_of(args[5], recent))
+        return slow();
+    const at::Tensor *mass = plain_on(c->device, args[0], at::kFloat);
+    const bool fresh = args[6] == Py_None;
+    const at::Tensor *given = fresh ? nullptr : plain_on(c->device, args[6], at::kInt);
+    if (!mass || !streams_of(c, *mass, batch) || (!fresh && (!given || given->dim() != 1 || given->size(0) != sequences(batch))) ||
+        !current_stream(c->device, s))
+        return slow();
+    const at::TensorOptions options = at::TensorOptions().dtype(at::kInt).device(c->device);
+    const at::Tensor kept = at::empty({sequences(batch), c->kv_heads, keep}, options);
+    const at::Tensor count = fresh ? at::empty({sequences(batch)}, options) : *given;
+    const float *mp = static_cast<const float *>(mass->data_ptr());
+    int32_t *kp = static_cast<int32_t *>(kept.data_ptr()), *cp = static_cast<int32_t *>(count.data_ptr());
+    const int64_t tokens = mass->size(2);
+    const int code = unlocked([&] { return lib.fp4_select(c->handle, batch, mp, tokens, keep, nullptr, sinks, recent, kp, cp, s); });
+    PyObject *first = THPVariable_Wrap(kept), *second = fresh ? THPVariable_Wrap(count) : Py_NewRef(args[6]);
+    PyObject *both = first && second ? PyTuple_Pack(2, first, second) : nullptr;
+    Py_XDECREF(first);
+    Py_XDECREF(second);
+    return both ? answer(code, "kv_fp4_select", both) : nullptr;
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject *fp4_compact(FP4Calls *c, PyObject *const *args, Py_ssize_t n) {   // kept, n_kept, batch, its device, to, its device, mass, mass_out, stream
+    HANDLE_TH_ERRORS
+    void *s;
+    const void *batch, *to;
+    if (n != 9 || !c->handle || args[8] != Py_None || modes() || !batch_of(c, args[2], args[3], batch) || !batch_of(c, args[4], args[5], to) ||
+        sequences(batch) != sequences(to))
+        return slow();
+    const at::Tensor *kept = plain_on(c->device, args[0], at::kInt), *count = plain_on(c->device, args[1], at::kInt);
+    const bool weighed = args[6] != Py_None;
+    const at::Tensor *mass = weighed ? plain_on(c->device, args[6], at::kFloat) : nullptr;
+    const at::Tensor *out = weighed ? plain_on(c->device, args[7], at::kFloat) : nullptr;
+    if (!kept || !streams_of(c, *kept, batch) || kept->size(2) > INT32_MAX || !count || count->dim() != 1 || count->size(0) != sequences(batch) ||
+        (weighed && (!mass || !out || !streams_of(c, *mass, batch) || !streams_of(c, *out, batch))) || (!weighed && args[7] != Py_None) ||
+        !current_stream(c->device, s))
+        return slow();
+    const int32_t *kp = static_cast<const int32_t *>(kept->data_ptr()), *cp = static_cast<const int32_t *>(count->data_ptr());
+    const float *mp = weighed ? static_cast<const float *>(mass->data_ptr()) : nullptr;
+    float *op = weighed ? static_cast<float *>(out->data_ptr()) : nullptr;
+    const int64_t tokens = weighed ? mass->size(2) : 0, out_tokens = weighed ? out->size(2) : 0;
+    const int32_t keep = int32_t(kept->size(2));
+    const int code = unlocked([&] { return lib.fp4_compact(c->handle, batch, to, kp, keep, cp, mp, tokens, op, out_tokens, s); });
+    return answer(code, "kv_fp4_compact", Py_NewRef(args[7]));
+    END_HANDLE_TH_ERRORS
+}
+
+// ---- rotary positions (binding.Rotary) ----
+
+struct RotaryCalls {
+    PyObject_HEAD
+    const void *table;       // kv_rotary_t, the caller's
+    int64_t head_dim;
+    c10::Device device;
+};
+
+// [rows, heads, head_dim] of `type`, the heads of a row next to each other.
+bool turned_rows(const RotaryCalls *c, PyObject *o, c10::ScalarType type, Rows &out) {
+    if (!THPVariable_CheckExact(o)) return false;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (t.layout() != c10::kStrided || t.scalar_type() != type || t.dim() != 3 || t.device() != c->device || t.size(2) != c->head_dim ||
+        t.stride(2) != 1 || (t.size(1) > 1 && t.stride(1) != c->head_dim) || t.is_conj() || t.is_neg())
+        return false;
+    out = {&t, t.size(0), t.size(0) > 1 ? t.stride(0) : t.size(1) * c->head_dim};
+    return true;
+}
+
+PyObject *rotary_turn(RotaryCalls *c, PyObject *const *args, Py_ssize_t n) {   // q, positions, k, out, k_out, inverse, stream
+    HANDLE_TH_ERRORS
+    void *s;
+    if (n != 7 || args[6] != Py_None || modes() || !THPVariable_CheckExact(args[0]) || (args[5] != Py_True && args[5] != Py_False)) return slow();
+    const c10::ScalarType type = THPVariable_Unpack(args[0]).scalar_type();
+    if (type != at::kHalf && type != at::kBFloat16 && type != at::kFloat) return slow();
+    const bool both = args[2] != Py_None;
+    Rows in[2], to[2];
+    if (!turned_rows(c, args[0], type, in[0]) || (both && !turned_rows(c, args[2], type, in[1])) || (!both && args[4] != Py_None)) return slow();
+    const at::Tensor *positions = plain_on(c->device, args[1], at::kInt);
+    if (!positions || positions->dim() != 1 || positions->size(0) != in[0].rows || (both && in[1].rows != in[0].rows)) return slow();
+    at::Tensor made[2];
+    for (int i = 0; i < (both ? 2 : 1); ++i) {
+        if (args[3 + i] != Py_None) {
+            if (!turned_rows(c, args[3 + i], type, to[i]) || to[i].t->sizes() != in[i].t->sizes()) return slow();
+        }
+    }
+    if (!current_stream(c->device, s)) return slow();
+    for (int i = 0; i < (both ? 2 : 1); ++i) {
+        if (args[3 + i] != Py_None) continue;
+        made[i] = at::empty(in[i].t->sizes(), at::TensorOptions().dtype(type).device(c->device));
+        to[i] = {&made[i], in[i].rows, in[i].t->size(1) * c->head_dim};
+    }
+    const void *from[2] = {in[0].t->data_ptr(), both ? in[1].t->data_ptr() : nullptr};
+    void *into[2] = {to[0].t->data_ptr(), both ? to[1].t->data_ptr() : nullptr};
+    const int32_t heads[2] = {int32_t(in[0].t->size(1)), both ? int32_t(in[1].t->size(1)) : 0};
+    const int32_t *at = static_cast<const int32_t *>(positions->data_ptr());
+    const int32_t inverse = args[5] == Py_True;
+    const int code = unlocked([&] {
+        return lib.rotary(c->table, at, in[0].rows, type_of(type), inverse, from[0], in[0].pitch, heads[0], into[0], to[0].pitch, from[1],
+                          both ? in[1].pitch : 0, heads[1], into[1], both ? to[1].pitch : 0, s);
+    });
+    PyObject *first = args[3] == Py_None ? THPVariable_Wrap(made[0]) : Py_NewRef(args[3]);
+    if (!both) return first ? answer(code, "kv_rotary", first) : nullptr;
+    PyObject *second = args[4] == Py_None ? THPVariable_Wrap(made[1]) : Py_NewRef(args[4]);
+    PyObject *pair = first && second ? PyTuple_Pack(2, first, second) : nullptr;
+    Py_XDECREF(first);
+    Py_XDECREF(second);
+    return pair ? answer(code, "kv_rotary", pair) : nullptr;
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject *rotary_calls_new(PyTypeObject *type, PyObject *args, PyObject *) {   // address of the kv_rotary_t, head_dim, device
+    HANDLE_TH_ERRORS
+    unsigned long long table;
+    long long head_dim;
+    const char *device;
+    if (!PyArg_ParseTuple(args, "KLs", &table, &head_dim, &device)) return nullptr;
+    const c10::Device d{std::string(device)};
+    RotaryCalls *c = reinterpret_cast<RotaryCalls *>(type->tp_alloc(type, 0));
+    if (!c) return nullptr;
+    c->table = reinterpret_cast<const void *>(uintptr_t(table));
+    c->head_dim = head_dim;
+    c->device = d;
+    return reinterpret_cast<PyObject *>(c);
     END_HANDLE_TH_ERRORS
 }
 
@@ -372,11 +575,16 @@ PyMethodDef calls_methods[] = {
 
 #define FAST_FP4(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fp4_##name)), METH_FASTCALL, nullptr}
 PyMethodDef fp4_calls_methods[] = {
-    FAST_FP4(append), FAST_FP4(read), FAST_FP4(attention),
+    FAST_FP4(append), FAST_FP4(read), FAST_FP4(read_into), FAST_FP4(attention), FAST_FP4(weights), FAST_FP4(select), FAST_FP4(compact),
     {"set_handle", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fp4_set_handle)), METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
-PyTypeObject calls_type = {PyVarObject_HEAD_INIT(nullptr, 0)}, fp4_calls_type = {PyVarObject_HEAD_INIT(nullptr, 0)};
+PyMethodDef rotary_calls_methods[] = {
+    {"turn", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rotary_turn)), METH_FASTCALL, nullptr},
+    {nullptr, nullptr, 0, nullptr}};
+
+PyTypeObject calls_type = {PyVarObject_HEAD_INIT(nullptr, 0)}, fp4_calls_type = {PyVarObject_HEAD_INIT(nullptr, 0)},
+             rotary_calls_type = {PyVarObject_HEAD_INIT(nullptr, 0)};
 
 // bind(addresses of the entry points in Library's order, _check, device getter, stream getter, bad-fork test)
 PyObject *bind(PyObject *, PyObject *args) {
@@ -413,10 +621,16 @@ PyMODINIT_FUNC PyInit__native() {
     fp4_calls_type.tp_flags = Py_TPFLAGS_DEFAULT;
     fp4_calls_type.tp_new = fp4_calls_new;
     fp4_calls_type.tp_methods = fp4_calls_methods;
-    if (PyType_Ready(&calls_type) < 0 || PyType_Ready(&fp4_calls_type) < 0) return nullptr;
+    rotary_calls_type.tp_name = "paper_2512_24449_amd._native.RotaryCalls";
+    rotary_calls_type.tp_basicsize = sizeof(RotaryCalls);
+    rotary_calls_type.tp_flags = Py_TPFLAGS_DEFAULT;
+    rotary_calls_type.tp_new = rotary_calls_new;
+    rotary_calls_type.tp_methods = rotary_calls_methods;
+    if (PyType_Ready(&calls_type) < 0 || PyType_Ready(&fp4_calls_type) < 0 || PyType_Ready(&rotary_calls_type) < 0) return nullptr;
     PyObject *m = PyModule_Create(&module);
     if (m && (PyModule_AddObject(m, "Calls", Py_NewRef(reinterpret_cast<PyObject *>(&calls_type))) < 0 ||
-              PyModule_AddObject(m, "FP4Calls", Py_NewRef(reinterpret_cast<PyObject *>(&fp4_calls_type))) < 0)) {
+              PyModule_AddObject(m, "FP4Calls", Py_NewRef(reinterpret_cast<PyObject *>(&fp4_calls_type))) < 0 ||
+              PyModule_AddObject(m, "RotaryCalls", Py_NewRef(reinterpret_cast<PyObject *>(&rotary_calls_type))) < 0)) {
         Py_DECREF(m);
         return nullptr;
     }
