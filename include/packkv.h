@@ -407,7 +407,7 @@ typedef struct {
 /* Bytes of the two device buffers of a cache. */
 typedef struct {
     size_t pages;     /* n_pages * n_kv_heads * 64 * (head_dim + head_dim / 16)   */
-    size_t workspace; /* partial results of attention                             */
+    size_t workspace; /* partial results of attention, weights and selection      */
 } kv_fp4_sizes_t;
 
 /* A ragged batch: sequence b holds lens[b] tokens, the last new_rows[b] of which
@@ -492,8 +492,8 @@ int kv_fp4_attention(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, const v
  * size, mass itself or not overlapping it; it is not read for the call's own tokens, positions from lens - new_rows on, which
  * no earlier row has seen.  A token that no row sees, and one of a missing page, keeps past's.  max_new may be 0: mass is then past.
  * fp32 throughout, q.Khat as in attention; what lse is off by (a few 2^-24 of its size) is a factor of a row's weights.  A row whose lse is
- * -infinity gives nothing, one whose q or lse is NaN makes the tokens that it sees NaN.  Sums have a fixed order.  Does not use the
- * workspace.
+ * -infinity gives nothing, one whose q or lse is NaN makes the tokens that it sees NaN.  Sums have a fixed order: the result is bitwise
+ * reproducible.  Uses the workspace: calls of kv_fp4_attention, kv_fp4_weights and kv_fp4_select on one cache must not overlap.
  */
 int kv_fp4_weights(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, const void *q, int64_t q_stride, int32_t type,
                    int64_t n_rows, float sm_scale, int32_t window, int32_t sinks, const float *lse, const float *past,
@@ -505,6 +505,7 @@ int kv_fp4_weights(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, const voi
  * 0.  budgets: device int32 [batch], or null: keep of each; a budget above keep (1 or more) is keep, below 0 it is 0.
  * kept: device int32 [batch][H_kv][keep], the positions in ascending order, -1 behind them; n_kept: device int32 [batch],
  * how many: the least of lens, the table's room and the budget.  Of the batch lens and table_pages are used; pages are not read.
+ * Uses the workspace, as kv_fp4_weights does.
  */
 int kv_fp4_select(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, const float *mass, int64_t mass_tokens, int32_t keep,
                   const int32_t *budgets, int32_t sinks, int32_t recent, int32_t *kept, int32_t *n_kept, void *hip_stream);

@@ -101,7 +101,7 @@ __global__ __launch_bounds__(SELECT_THREADS, 4) void fp4_select_kernel(Fp4Select
     const float *mass = a.mass + stream * a.pitch;
     int32_t *kept = a.kept + stream * a.keep;
     if (h == 0 && tid == 0) a.n_kept[b] = r.n;
-    for (int i = r.n + tid; i < a.keep; i += SELECT_THREADS) kept[i] = -1;
+    for (int64_t i = r.n + tid; i < a.keep; i += SELECT_THREADS) kept[i] = -1;
     if (r.len <= r.budget) {
         for (int i = tid; i < r.n; i += SELECT_THREADS) kept[i] = i;
         return;
@@ -263,7 +263,7 @@ __global__ __launch_bounds__(SELECT_THREADS) void fp4_select_long_kernel(Fp4Sele
     const float *mass = a.mass + stream * a.pitch;
     int32_t *kept = a.kept + stream * a.keep;
     if (h == 0 && tid == 0) a.n_kept[b] = r.n;
-    for (int i = r.n + tid; i < a.keep; i += SELECT_THREADS) kept[i] = -1;
+    for (int64_t i = r.n + tid; i < a.keep; i += SELECT_THREADS) kept[i] = -1;
     if (r.len <= r.budget) {
         for (int i = tid; i < r.n; i += SELECT_THREADS) kept[i] = i;
         return;

@@ -155,9 +155,9 @@ extern "C" int kv_rotary(const kv_rotary_t *rotary, const int32_t *positions, in
     r.units = (in_place ? dims : D) / (2 * width);
     r.slots = 256 / r.units;
     r.splits = int(std::min<int64_t>(r.heads, std::max<int64_t>(ROTARY_SPLITS, ROTARY_SLOTS / n_rows)));
-    const bool streamed = n_rows * r.heads * int64_t(D) * int64_t(size) >= ROTARY_STREAMED;
     const int64_t groups = (n_rows * r.splits + r.slots - 1) / r.slots;
     if (n_rows > (int64_t(1) << 40) || groups > (int64_t(1) << 24) - 1) return KV_ERR_UNSUPPORTED;
+    const bool streamed = n_rows * r.heads * int64_t(D) * int64_t(size) >= ROTARY_STREAMED;
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
     const bool i = rotary->interleaved != 0;
 #define WIDTHS(T)                                                    \

@@ -185,6 +185,52 @@ def test_queries_in_parts_of_wider_rows():
     assert torch.equal(held.cache.kv_fp4_weights(q, lse, batch, 0.1), held.cache.kv_fp4_weights(q.contiguous(), lse, batch, 0.1))
 
 
+def test_weights_of_several_pages_to_a_wave():
+    """Wide tables: what a wave takes follows the table's width; pages that rows see and do not see in turn."""
+    for lens, new, G in (([3000, 700], [1, 1], 2), ([3000, 700], [20, 9], 3)):
+        held = Filled(lens, 2, G, 64, torch.float16, 28, extra=4000)
+        check_weights(held, new)
+        check_weights(held, new, window=300, sinks=70, seed=52)
+        check_weights(held, new, window=1, past=False, seed=53)
+
+
+def check_long(tokens, new, dim=64):
+    """One head, values that repeat: what the cache holds by kv_fp4_read, scores in 64 bits on the GPU."""
+    gen = torch.Generator(device=DEV).manual_seed(54)
+    k = torch.randn(tokens, 1, dim, generator=gen, device=DEV).half()
+    n_pages = -(-tokens // 64)
+    cache = binding.FP4KVCache(n_pages, 1, 1, dim)
+    batch = binding.FP4Batch(ints([tokens]), tokens, table_pages=n_pages)
+    cache.kv_fp4_append(k, k, batch)
+    values = cache.kv_fp4_read(batch, tokens, torch.float16)[0][:, 0]
+    q = torch.randn(new, 1, dim, generator=gen, device=DEV).half()
+    rows_of = binding.FP4Batch(ints([tokens]), new, table_pages=n_pages)
+    lse = torch.empty(new, 1, device=DEV)
+    cache.kv_fp4_attention(q, rows_of, 0.1, lse=lse)
+    got = cache.kv_fp4_weights(q, lse, rows_of, 0.1)
+    want, bound = torch.zeros(tokens, dtype=torch.float64, device=DEV), torch.zeros(tokens, dtype=torch.float64, device=DEV)
+    t = torch.arange(tokens, device=DEV)
+    for i in range(new):                                         # (the bound of budget_reference.weights)
+        s = values.double() @ q[i, 0].double() * 0.1
+        size = values.double().abs() @ q[i, 0].double().abs() * 0.1
+        p = torch.where(t <= tokens - new + i, torch.exp(s - lse[i, 0].double()), 0.0)
+        want += p
+        bound += p * torch.expm1((dim + 8) * ref.STEP * size + 3 * ref.STEP * (s.abs() + lse[i, 0].double().abs()) + 2 * ref.STEP)
+    bound += (new + 2) * ref.STEP * want + new * 2.0 ** -126
+    assert bool(((got[0, 0, :tokens].double() - want).abs() <= bound).all())
+    return cache, got, rows_of
+
+
+def test_more_pages_than_a_launch_has_workgroups_for():
+    check_long(1_100_000, 200)
+    cache, mass, batch = check_long(6_400_001, 1)
+    kept, count = cache.kv_fp4_select(mass, batch, 100_000, 4, 1000)
+    middle = mass[0, 0, 4:6_400_001 - 1000].double()
+    most = torch.sort(-middle, stable=True).indices[:100_000 - 1004] + 4
+    want = torch.cat([most, torch.arange(4, device=DEV), torch.arange(6_400_001 - 1000, 6_400_001, device=DEV)]).sort().values
+    assert torch.equal(kept[0, 0].long(), want) and int(count) == 100_000
+
+
 # ---- which tokens are kept ----
 
 def heavy(shape, seed, zeros=0.2):

@@ -165,3 +165,13 @@ def test_captured_and_on_another_stream():
         torch.cuda.synchronize()
         assert torch.equal(a, want[0]) and torch.equal(b, want[1])
         check(rotary, a, q, p)
+
+
+def test_keys_alone_through_the_library():
+    rotary = binding.Rotary(64, 32)
+    k, p = rows(9, 3, 64, torch.float16, 19), positions(9, 20)
+    x, at, out = k.to(DEV), p.to(DEV), torch.empty(9, 3, 64, dtype=torch.float16, device=DEV)
+    rc = binding.lib().kv_rotary(rotary._ref, at.data_ptr(), 9, binding.KV_TYPE_FP16, 1, None, 0, 0, None, 0, x.data_ptr(), 192, 3, out.data_ptr(), 192,
+                                 torch.cuda.current_stream().cuda_stream)
+    assert rc == 0
+    check(rotary, out, k, p, inverse=True)
