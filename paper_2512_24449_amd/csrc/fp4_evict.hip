@@ -300,7 +300,8 @@ __global__ __launch_bounds__(SELECT_THREADS) void fp4_select_long_kernel(Fp4Sele
     each([&](int t, uint32_t key) { write_kept(kept, t, sure(t, key), tie(t, key), wanted, at, tied, lane); });
 }
 
-// Long sequences of few heads, a workgroup to SELECT_PART tokens, in three launches: counts of the first digit of every part; that
+// Long sequences, a workgroup to SELECT_PART tokens, in three launches (8 heads of 131079 tokens 21.5 us, 4 + 8 + 10 in the kernels; a
+// workgroup to each, reading again for every digit, 163): counts of the first digit of every part; that
 // digit from all parts' counts, and each part's keys with it; the other digits from those keys -- every workgroup for
 // itself -- and the positions.  What the parts hand on of a (sequence, kv-head): counts [parts][2048], keys
 // [parts][SELECT_PART], tokens above the digit [parts] and keys [parts], the digit and how many are wanted of it.
@@ -480,6 +481,8 @@ __global__ __launch_bounds__(SELECT_THREADS) void fp4_select_part_kernel(Fp4Sele
     }
 }
 
+// Which kernel goes by the table's room.  Keys of up to 40960 tokens fit a workgroup's registers: four sequences of up to 32788 tokens, 8
+// heads, selected, moved and read back so / in parts 91 / 100 us.  Beyond, parts, where the workspace holds what they hand on.
 int launch_fp4_select(const kv_fp4_cache *c, Fp4Select a, hipStream_t s) {
     const int64_t room = int64_t(a.v.batch.table_pages) * FP4_PAGE, streams = int64_t(a.v.H) * a.v.batch.batch;
     a.parts = int((room + SELECT_PART - 1) / SELECT_PART);
@@ -517,8 +520,12 @@ struct Fp4Compact {
 // A wave to some eights of tokens of a kv-head where they go, the next eight on its way while one is written: a word of V's channels there
 // takes a code from each of eight words, HD / 64 channels to a lane; K's rows are 8 (4) bytes to a lane.  Where
 // the tokens come from -- positions, then page numbers -- is found for all of them at once, a token to a lane.
-constexpr int COMPACT_EIGHTS = 4;        // at most: 32 tokens
-constexpr int64_t COMPACT_WAVES = 8192;
+// Bound by HBM and the chain of latencies before the first row (lengths, positions, page numbers): 4 x 8 heads, 8197 of up to 32788
+// tokens each, in 31 us (some 120 MB: a quarter of the tokens touches nearly all of V's groups of eight and half of K's lines).
+// Eights to a wave: one to each of so many waves first, then up to eight, a token to a lane.  Selected, moved and read back, that cut
+// with 1 / 2 / 4 / 8 eights to a wave 99.4 / 91.9 / 90.3 / 87.4 us, one of 1000 tokens to 200 16.7 / 17.4 / 18.5 / 24.1.
+constexpr int COMPACT_EIGHTS = 8;
+constexpr int64_t COMPACT_WAVES = 4096;
 template <int HD>
 struct Fp4Eight {
     using P = Fp4Block<HD>;
@@ -633,8 +640,8 @@ extern "C" int kv_fp4_compact(kv_fp4_cache_t *c, const kv_fp4_batch_t *from, con
     if (!mass != !mass_out) return KV_ERR_ARG;
     if (mass && (mass_tokens < 1 || mass_out_tokens < 1 || !fp4_aligned(mass, 4) || !fp4_aligned(mass_out, 4))) return KV_ERR_ARG;
     const Fp4Compact a{fp4_view(c, from, 0), fp4_view(c, to, 0), kept, n_kept, keep, mass, mass_tokens, mass_out, mass_out_tokens};
-    // several eights to a wave where there are more waves than run at once
-    const int64_t eights = (int64_t(keep) + 7) / 8, each = eights * c->cfg.n_kv_heads * from->batch >= COMPACT_WAVES ? COMPACT_EIGHTS : 1;
+    const int64_t eights = (int64_t(keep) + 7) / 8;
+    const int64_t each = std::max<int64_t>(std::min<int64_t>(eights * c->cfg.n_kv_heads * from->batch / COMPACT_WAVES, COMPACT_EIGHTS), 1);
     const int64_t units = (eights + each - 1) / each, groups = (units * c->cfg.n_kv_heads + 3) / 4;
     if (groups > FP4_GROUPS_MOST) return KV_ERR_UNSUPPORTED;
     const dim3 grid = dim3(uint32_t(groups), uint32_t(from->batch));

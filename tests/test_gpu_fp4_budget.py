@@ -367,6 +367,37 @@ def test_compact(lens, H, D, keep, dtype):
     assert held.cache.kv_fp4_compact(kept.to(DEV), count, held.batch([0] * B, max_new=0), to) is None
 
 
+@pytest.mark.parametrize("B, H, D, keep", [(4, 8, 64, 2603), (8, 8, 128, 4101), (3, 30, 64, 1441)])
+def test_compact_of_many_tokens(B, H, D, keep):
+    """Several eights to a wave, ends inside them, tokens that are not there among them: against what reading back and gathering give."""
+    gen = torch.Generator(device=DEV).manual_seed(33)
+    lens = [keep + 1500 - 37 * b for b in range(B)]
+    most, kept_pages = max(lens), -(-keep // 64)
+    pages = -(-most // 64)
+    cache = binding.FP4KVCache(B * (pages + kept_pages), H, H, D)
+    order = torch.randperm(B * (pages + kept_pages), generator=gen, device=DEV).int()
+    table, to_table = order[:B * pages].view(B, pages).contiguous(), order[B * pages:].view(B, kept_pages).contiguous()
+    n = ints(lens)
+    whole = binding.FP4Batch(n, most, table, new_rows=n)
+    k, v = (torch.randn(B * most, H, D, generator=gen, device=DEV).half() for _ in range(2))
+    cache.kv_fp4_append(k, v, whole)
+    held = [x.view(B, most, H, D) for x in cache.kv_fp4_read(whole, B * most)]
+    kept = torch.randint(0, most + 20, (B, H, keep), generator=gen, device=DEV, dtype=torch.int32)   # (some behind the end)
+    count = ints([keep - 5 * b for b in range(B)])
+    to = binding.FP4Batch(count, keep, to_table, new_rows=count)
+    mass = torch.rand(B, H, most, generator=gen, device=DEV)
+    moved = cache.kv_fp4_compact(kept, count, whole, to, mass=mass)
+    out = [x.view(B, keep, H, D) for x in cache.kv_fp4_read(to, B * keep)]
+    for b in range(B):
+        m = keep - 5 * b
+        there = kept[b, :, :m] < lens[b]
+        index = kept[b, :, :m].clamp(max=lens[b] - 1).long()
+        assert torch.equal(moved[b, :, :m], torch.where(there, mass[b].gather(1, index), 0.0)) and bool((moved[b, :, m:] == 0).all())
+        for x, y in zip(held, out):
+            want = x[b].gather(0, index.T[..., None].expand(-1, -1, D))
+            assert torch.equal(y[b, :m], torch.where(there.T[..., None], want, torch.zeros_like(want)))
+
+
 def test_compact_of_odd_positions():
     """Out of order, the same twice, not there, of a missing page; to a missing page; fewer and more than there is room for."""
     held = Filled([300, 100], 2, 1, 128, torch.float16, 32, more_pages=6)
