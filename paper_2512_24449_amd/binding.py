@@ -666,7 +666,7 @@ class FP4KVCache(_Operators):
 
     def kv_fp4_weights(self, q, lse, batch, sm_scale, window=0, sinks=0, past=None, out=None, stream=None):
         """The attention weight that every cached token gets from the batch's new rows, on top of `past`: fp32 [batch, H_kv, tokens].
-        q, sm_scale, window and sinks as kv_fp4_attention had them, lse as it gave them; past: null, or of out's shape, or out
+        q, sm_scale, window and sinks as kv_fp4_attention had them, lse as it gave them; past: of out's shape, or out
         itself; it counts for the tokens before the new rows.  Without out a new tensor of past's shape, or of the page table's
         width, zeros where the sequences have no tokens; places of out behind a sequence's tokens are not written."""
         if out is not None:

@@ -442,13 +442,12 @@ constexpr int64_t WEIGHTS_GROUPS = 2304;
 int launch_fp4_weights(const kv_fp4_cache *c, const Fp4View &v, const void *q, int64_t q_stride, bool bf16, float sm_scale, int window,
                        int sinks, const float *lse, const float *past, float *mass, int64_t mass_tokens, hipStream_t s) {
     Fp4Weights a{v, static_cast<const uint16_t *>(q), q_stride, lse, sm_scale * FP4_LOG2E, window, sinks,
-                       past, mass, mass_tokens, nullptr, 1};
+                 past, mass, mass_tokens, nullptr, 1};
     const int64_t columns = int64_t(v.batch.max_new) * v.G, most = int64_t(v.batch.table_pages) * v.H * v.batch.batch;   // pages
     const bool tiles = columns > 16 * WEIGHTS_HELD;
     const int each = tiles ? 1 : int(std::max<int64_t>(columns > 16 ? std::min<int64_t>((most + WEIGHTS_ROUND - 1) / WEIGHTS_ROUND, 64)
                                                                     : std::min<int64_t>(most / WEIGHTS_ROUND, WEIGHTS_PAGES), 1));
-    const int64_t groups = std::min<int64_t>((v.batch.table_pages + 4 * each - 1) / (4 * each), 4096);
-    if (groups * v.H > FP4_GROUPS_MOST) return KV_ERR_UNSUPPORTED;
+    const int64_t groups = std::min({(v.batch.table_pages + int64_t(4) * each - 1) / (4 * each), int64_t(4096), FP4_GROUPS_MOST / v.H});
     if (tiles) {
         const int64_t room = FP4_PART_ROWS * (c->cfg.head_dim + 4) / (most * FP4_PAGE), stages = (columns + 63) / 64;
         a.splits = int(std::max<int64_t>(std::min({WEIGHTS_GROUPS / (groups * v.H * v.batch.batch), room, stages / 4, int64_t(64)}), 1));
