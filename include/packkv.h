@@ -489,7 +489,7 @@ int kv_fp4_attention(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, const v
  * with q, sm_scale, window, sinks (and so which rows see t) and lse as the call of kv_fp4_attention on the same batch had or
  * gave them.  mass: device fp32 [batch][H_kv][mass_tokens]; written are the places of the tokens that the sequence holds
  * (and the page table and mass have room for), others are left as they were.  past: null (0), or of mass's
- * size, mass itself or not overlapping it; it is not read for the call's own tokens, positions from lens - new_rows on, which
+ * size, mass itself or not overlapping it (mass overlaps nothing else that the call reads: KV_ERR_ARG); it is not read for the call's own tokens, positions from lens - new_rows on, which
  * no earlier row has seen.  A token that no row sees, and one of a missing page, keeps past's.  max_new may be 0: mass is then past.
  * fp32 throughout, q.Khat as in attention; what lse is off by (a few 2^-24 of its size) is a factor of a row's weights.  A row whose lse is
  * -infinity gives nothing, one whose q or lse is NaN makes the tokens that it sees NaN.  Sums have a fixed order: the result is bitwise
@@ -505,6 +505,7 @@ int kv_fp4_weights(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, const voi
  * 0.  budgets: device int32 [batch], or null: keep of each; a budget above keep (1 or more) is keep, below 0 it is 0.
  * kept: device int32 [batch][H_kv][keep], the positions in ascending order, -1 behind them; n_kept: device int32 [batch],
  * how many: the least of lens, the table's room and the budget.  Of the batch lens and table_pages are used; pages are not read.
+ * kept and n_kept overlap neither each other nor lens, mass or budgets (KV_ERR_ARG): sequences whose lens are an n_kept are cut into another one.
  * Uses the workspace, as kv_fp4_weights does.
  */
 int kv_fp4_select(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, const float *mass, int64_t mass_tokens, int32_t keep,
@@ -517,7 +518,8 @@ int kv_fp4_select(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, const floa
  * what would go to a page that is missing is left out.  Its lens are not read (they may be n_kept itself: the batch of the sequences
  * from then on).  In the group of eight tokens that the last one is in, those behind it become zeros.
  * mass, mass_out: both null, or device fp32 [batch][H_kv][mass_tokens] and, not overlapping, [batch][H_kv][mass_out_tokens]: weights that go with
- * the tokens (0 of a token that mass has no room for); places from n_kept on are left as they were.
+ * the tokens (0 of a token that mass has no room for); places from n_kept on are left as they were.  mass_out overlaps nothing that the call
+ * reads (KV_ERR_ARG).
  * From then on a token's position in the cache is no longer its position in the text: rotary positions of later rows count on
  * from the text's.
  */

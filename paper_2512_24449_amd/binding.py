@@ -696,7 +696,8 @@ class FP4KVCache(_Operators):
     def kv_fp4_select(self, mass, batch, keep, sinks=0, recent=0, budgets=None, kept=None, n_kept=None, stream=None):
         """Which tokens the batch's sequences keep, of mass [batch, H_kv, tokens] (kv_fp4_weights): (kept, n_kept), int32 [batch, H_kv,
         keep], positions in ascending order and -1 behind them, and int32 [batch].  All of a sequence of no more than keep (or
-        budgets[b], int32 [batch]) tokens; else the first `sinks`, the last `recent` and the others of the largest mass."""
+        budgets[b], int32 [batch]) tokens; else the first `sinks`, the last `recent` and the others of the largest mass.  kept, n_kept: where to;
+        not the batch's lens, which the call reads."""
         if budgets is None and kept is None:
             done = self._calls.select(mass, batch._address, batch._on, keep, sinks, recent, n_kept, stream)
             if done is not NotImplemented:

@@ -3,6 +3,7 @@
 #include <type_traits>
 
 #include "fp4.h"
+#include "overlap.h"
 #include "unpack.h"
 
 namespace packkv {
@@ -629,6 +630,10 @@ extern "C" int kv_fp4_select(kv_fp4_cache_t *c, const kv_fp4_batch_t *batch, con
     if (rc) return rc;
     if (mass_tokens < 1 || keep < 1 || sinks < 0 || recent < 0) return KV_ERR_ARG;
     if (!fp4_aligned(mass, 4) || !fp4_aligned(kept, 4) || !fp4_aligned(n_kept, 4) || (budgets && !fp4_aligned(budgets, 4))) return KV_ERR_ARG;
+    const int64_t streams = int64_t(batch->batch) * c->cfg.n_kv_heads;
+    const Rows lens(batch->lens, batch->batch, 4), weights(mass, Rows::Wide(streams) * mass_tokens, 4), most(budgets, batch->batch, 4),
+        positions(kept, Rows::Wide(streams) * keep, 4), counts(n_kept, batch->batch, 4);
+    if (overlap(positions, {lens, weights, most, counts}) || overlap(counts, {lens, weights, most})) return KV_ERR_ARG;
     return launch_fp4_select(c, Fp4Select{fp4_view(c, batch, 0), mass, mass_tokens, keep, sinks, recent, budgets, kept, n_kept, nullptr, 0},
                              static_cast<hipStream_t>(hip_stream));
 }
@@ -642,6 +647,12 @@ extern "C" int kv_fp4_compact(kv_fp4_cache_t *c, const kv_fp4_batch_t *from, con
     if (from->batch != to->batch || keep < 1 || !fp4_aligned(kept, 4) || !fp4_aligned(n_kept, 4)) return KV_ERR_ARG;
     if (!mass != !mass_out) return KV_ERR_ARG;
     if (mass && (mass_tokens < 1 || mass_out_tokens < 1 || !fp4_aligned(mass, 4) || !fp4_aligned(mass_out, 4))) return KV_ERR_ARG;
+    const int64_t streams = int64_t(from->batch) * c->cfg.n_kv_heads;
+    if (overlap(Rows(mass_out, Rows::Wide(streams) * mass_out_tokens, 4),
+                {Rows(mass, Rows::Wide(streams) * mass_tokens, 4), Rows(kept, Rows::Wide(streams) * keep, 4), Rows(n_kept, from->batch, 4),
+                 Rows(from->lens, from->batch, 4), Rows(from->page_table, int64_t(from->batch) * from->table_pages, 4),
+                 Rows(to->page_table, int64_t(to->batch) * to->table_pages, 4)}))
+        return KV_ERR_ARG;
     const Fp4Compact a{fp4_view(c, from, 0), fp4_view(c, to, 0), kept, n_kept, keep, mass, mass_tokens, mass_out, mass_out_tokens};
     const int64_t eights = (int64_t(keep) + 7) / 8;
     const int64_t each = std::max<int64_t>(std::min<int64_t>(eights * c->cfg.n_kv_heads * from->batch / COMPACT_WAVES, COMPACT_EIGHTS), 1);

@@ -13,6 +13,7 @@
 // large library product reaches 1345; per 16 columns and page 68 vector instructions, 16 of them exponentials of four times the
 // cost, beside 16 products: vector instructions are issued 72 % of the time, the matrix cores are busy 40 %.
 #include "fp4_attention.h"
+#include "overlap.h"
 
 namespace packkv {
 
@@ -491,6 +492,12 @@ extern "C" int kv_fp4_weights(kv_fp4_cache_t *c, const kv_fp4_batch_t *batch, co
     if (mass_tokens < 1 || !fp4_aligned(mass, 4) || (past && !fp4_aligned(past, 4))) return KV_ERR_ARG;
     if (n_rows > 0 && batch->max_new > 0 && (!fp4_aligned(q, 16) || !fp4_aligned(lse, 4))) return KV_ERR_ARG;
     if (int64_t(batch->max_new) * (c->cfg.n_q_heads / c->cfg.n_kv_heads) > (int64_t(1) << 30)) return KV_ERR_UNSUPPORTED;
+    const int64_t n = batch->batch, columns = c->cfg.n_q_heads, places = n * c->cfg.n_kv_heads, rows = batch->max_new > 0 ? n_rows : 0;
+    const Rows written(mass, Rows::Wide(places) * mass_tokens, 4);
+    if (overlap(written, {Rows(mass == past ? nullptr : past, Rows::Wide(places) * mass_tokens, 4), Rows(lse, Rows::Wide(rows) * columns, 4),
+                          Rows(q, columns * c->cfg.head_dim * 2, Rows::Wide(q_stride) * 2, rows), Rows(batch->lens, n, 4),
+                          Rows(batch->new_rows, n, 4), Rows(batch->first_row, n, 4), Rows(batch->page_table, n * batch->table_pages, 4)}))
+        return KV_ERR_ARG;
     return launch_fp4_weights(c, fp4_view(c, batch, n_rows), q, q_stride, type == KV_TYPE_BF16, sm_scale, window, sinks, lse, past, mass,
                               mass_tokens, static_cast<hipStream_t>(hip_stream));
 }

@@ -1,0 +1,43 @@
+"""Calls around a cache's budget at the edges of what they write and take."""
+import pytest
+import torch
+
+from paper_2512_24449_amd import binding
+from tests.test_gpu_fp4_budget import Filled, ints, query
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def test_tensors_next_to_each_other_in_one_buffer():
+    """What a call writes may begin where what it reads ends."""
+    held = Filled([500, 300], 2, 4, 128, torch.float16, 70, more_pages=4)
+    q = query(6, 8, 128, torch.float16, 71)
+    shapes = dict(past=(2, 2, 500), mass=(2, 2, 500), n_kept=(2,), budgets=(2,), kept=(2, 2, 100), lse=(6, 8), mass_out=(2, 2, 77), lens=(2,))
+    place, at = {}, 0
+    for name, shape in shapes.items():
+        n = torch.Size(shape).numel()
+        place[name] = (at, at + n, shape)
+        at += n
+
+    def together():
+        flat = torch.zeros(at, dtype=torch.int32, device=DEV)
+        t = {name: flat[a:b].view(shape) for name, (a, b, shape) in place.items()}
+        return {name: x if name in ("n_kept", "budgets", "kept", "lens") else x.view(torch.float32) for name, x in t.items()}
+
+    def apart():
+        return {name: x.clone() for name, x in together().items()}
+
+    results = []
+    for t in (together(), apart()):
+        t["past"].copy_(torch.rand(2, 2, 500, generator=torch.Generator().manual_seed(72)))
+        t["lens"].copy_(ints(held.lens)), t["budgets"].copy_(ints([90, 100]))
+        batch = binding.FP4Batch(t["lens"], 4, held.table, new_rows=ints([4, 2]), first_row=ints([0, 4]))
+        held.cache.kv_fp4_attention(q.to(DEV), batch, 0.1, lse=t["lse"])
+        held.cache.kv_fp4_weights(q.to(DEV), t["lse"], batch, 0.1, past=t["past"], out=t["mass"])
+        held.cache.kv_fp4_select(t["mass"], batch, 100, 4, 10, budgets=t["budgets"], kept=t["kept"], n_kept=t["n_kept"])
+        to = binding.FP4Batch(t["n_kept"], 100, held.n_pages + ints([[0, 1], [2, 3]]), new_rows=t["n_kept"])
+        held.cache.kv_fp4_compact(t["kept"], t["n_kept"], batch, to, mass=t["mass"], mass_out=t["mass_out"])
+        results.append(t)
+    assert results[0]["n_kept"].tolist() == [90, 100]
+    assert all(torch.equal(results[0][name], results[1][name]) for name in shapes)
