@@ -554,20 +554,18 @@ struct Fp4Eight {
             for (int c = 0; c < C; ++c) v[i][c] = words[c];
         }
     }
-    // out: the page's block; at: the first of the eight in it; n: how many there are
-    __device__ inline void store(uint8_t *out, int at, int n, int page, int slot, int eight, int lane) const {
+    // out: the page's block; at: the first of the eight in it.  All eight are written: those without a page, behind the last token too, as zeros.
+    __device__ inline void store(uint8_t *out, int at, int page, int slot, int eight, int lane) const {
         const int j = lane & 7, s = lane / 8;
         const bool there = __shfl(page, 8 * eight + j) >= 0;
-        if (s < SCALES && j < n) {
+        if (s < SCALES) {
             out[P::KS + (at + j) * SCALES + s] = there ? ks : uint8_t(127);
             out[P::VS + s * FP4_PAGE + at + j] = there ? vs : uint8_t(127);
         }
         const bool row = __shfl(page, 8 * eight + s) >= 0;
         uint32_t *to = reinterpret_cast<uint32_t *>(out + P::K + (at + s) * (HD / 2) + j * (HD / 16));
-        if (s < n) {
 #pragma unroll
-            for (int c = 0; c < C; ++c) to[c] = row ? k[c] : 0u;
-        }
+        for (int c = 0; c < C; ++c) to[c] = row ? k[c] : 0u;
         uint32_t word[C] = {};
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -606,7 +604,7 @@ __global__ __launch_bounds__(256) void fp4_compact_kernel(Fp4Compact a, int unit
     const auto store = [&](const Fp4Eight<HD> &x, int e) {
         const int to = __builtin_amdgcn_readlane(to_page, 8 * e);
         if (to < 0) return;
-        x.store(v.pages + (int64_t(to) * v.H + h) * size_t(P::BYTES), (i0 + 8 * e) % FP4_PAGE, min(here - 8 * e, 8), page, slot, e, lane);
+        x.store(v.pages + (int64_t(to) * v.H + h) * size_t(P::BYTES), (i0 + 8 * e) % FP4_PAGE, page, slot, e, lane);
     };
     Fp4Eight<HD> in[2];
     in[0].load(v, h, page, slot, 0, lane);

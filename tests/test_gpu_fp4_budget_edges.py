@@ -41,3 +41,25 @@ def test_tensors_next_to_each_other_in_one_buffer():
         results.append(t)
     assert results[0]["n_kept"].tolist() == [90, 100]
     assert all(torch.equal(results[0][name], results[1][name]) for name in shapes)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [[1, 9, 64], [7, 8, 15], [63, 65, 0], [121, 3, 127]])
+def test_compaction_clears_the_rest_of_the_last_eight(n, D):
+    """Tokens behind the last one, up to a whole eight, are zeros in pages that held anything; those of the next eight stay."""
+    lens, H, keep = [150, 140, 130], 2, 128
+    held = Filled(lens, H, 1, D, torch.float16, 73, more_pages=6)
+    page = H * 64 * (D + D // 16)
+    held.cache.pages[held.n_pages * page:] = 255
+    to_table = held.n_pages + ints([[3, 0], [5, 1], [2, 4]])
+    kept = torch.arange(keep, dtype=torch.int32, device=DEV).flip(0).expand(3, H, keep).contiguous()
+    count = ints(n)
+    held.cache.kv_fp4_compact(kept, count, held.batch([0] * 3, max_new=0), binding.FP4Batch(count, keep, to_table))
+    whole = binding.FP4Batch(ints([keep] * 3), keep, to_table)
+    for x, y in zip((held.k, held.v), held.cache.kv_fp4_read(whole, 3 * keep, torch.float32)):
+        y = y.cpu().double().view(3, keep, H, D)
+        for b, m in enumerate(n):
+            end = -(-m // 8) * 8
+            assert torch.equal(y[b, :m], x[b][kept[b, 0, :m].long().cpu()])
+            assert bool((y[b, m:end] == 0).all())
+            assert not torch.isfinite(y[b, end:]).any()          # (scales of 255 as they were)
