@@ -492,7 +492,7 @@ int kv_fp4_attention(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, const v
  * size, mass itself or not overlapping it (mass overlaps nothing else that the call reads: KV_ERR_ARG); it is not read for the call's own tokens, positions from lens - new_rows on, which
  * no earlier row has seen.  A token that no row sees, and one of a missing page, keeps past's.  max_new may be 0: mass is then past.
  * fp32 throughout, q.Khat as in attention; what lse is off by (a few 2^-24 of its size) is a factor of a row's weights.  A row whose lse is
- * -infinity gives nothing, one whose q or lse is NaN makes the tokens that it sees NaN.  Sums have a fixed order: the result is bitwise
+ * -infinity gives nothing, whatever its q is; another whose q (unless sm_scale is 0) or lse is NaN makes the tokens that it sees NaN.  Sums have a fixed order: the result is bitwise
  * reproducible.  Uses the workspace: calls of kv_fp4_attention, kv_fp4_weights and kv_fp4_select on one cache must not overlap.
  */
 int kv_fp4_weights(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, const void *q, int64_t q_stride, int32_t type,

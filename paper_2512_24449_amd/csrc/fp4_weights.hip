@@ -42,7 +42,7 @@ struct Fp4RowSet {
 };
 
 // A lane's part of 16 columns' operand on its way, and (lanes 0 .. 15) of what their rows need; then 64 columns further on.
-// An infinity in q needs no care: the row's lse is NaN then.
+// An infinity in q needs no care where its row counts: the row's lse is NaN then.
 template <int HD, bool BF16>
 struct Fp4Columns {
     static constexpr int KW = HD / 32;
@@ -74,10 +74,13 @@ struct Fp4Columns {
         of += rows64, beside += heads64;
         if (beside >= G) beside -= G, ++of;
     }
+    // 0 for q where there is no row, where its scores do not count and where the scale is 0: minus infinity added to an infinite score, or 0
+    // times it, is NaN.
     __device__ inline void settle(const Fp4Weights &a) {
-        if (__all(real) && a.scale != 0.0f) return;
+        const bool counts = real && lse != -INFINITY && a.scale != 0.0f;
+        if (__all(counts)) return;
 #pragma unroll
-        for (int i = 0; i < KW; ++i) q[i] = real && a.scale != 0.0f ? q[i] : uint4_t{0, 0, 0, 0};
+        for (int i = 0; i < KW; ++i) q[i] = counts ? q[i] : uint4_t{0, 0, 0, 0};
     }
     __device__ inline void store(Fp4RowSet &set, const Fp4Sequence &seq, int lane) const {
         const int hi = max(seq.pos0 + min(row, seq.n - 1), -1);

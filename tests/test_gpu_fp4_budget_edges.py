@@ -63,3 +63,20 @@ def test_compaction_clears_the_rest_of_the_last_eight(n, D):
             assert torch.equal(y[b, :m], x[b][kept[b, 0, :m].long().cpu()])
             assert bool((y[b, m:end] == 0).all())
             assert not torch.isfinite(y[b, end:]).any()          # (scales of 255 as they were)
+
+
+@pytest.mark.parametrize("new, G", [(3, 2), (20, 3), (50, 4)])   # one block of columns, some, many
+@pytest.mark.parametrize("dtype, value", [(torch.float16, float("inf")), (torch.float16, -float("inf")), (torch.bfloat16, float("nan")),
+                                          (torch.bfloat16, 3e38), (torch.bfloat16, -3e38)])
+def test_a_row_whose_logarithm_is_minus_infinity_gives_nothing(new, G, dtype, value):
+    """Whatever its query is: infinite, NaN, or finite with scores that are not."""
+    held = Filled([200], 2, G, 128, dtype, 74)
+    q = query(new, 2 * G, 128, dtype, 75).to(DEV)
+    batch = held.batch([new])
+    lse = torch.empty(new, 2 * G, device=DEV)
+    held.cache.kv_fp4_attention(q, batch, 0.1, lse=lse)
+    lse[1, 1] = lse[new - 1, 2 * G - 1] = -float("inf")
+    plain = held.cache.kv_fp4_weights(q, lse, batch, 0.1)
+    assert torch.isfinite(plain).all()
+    q[1, 1], q[new - 1, 2 * G - 1, ::3] = value, value
+    assert torch.equal(held.cache.kv_fp4_weights(q, lse, batch, 0.1), plain)
