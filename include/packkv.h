@@ -544,8 +544,8 @@ typedef struct {
 /*
  * positions: device int32 [n_rows], any values, read when the kernel runs.  q: device [n_rows][n_q_heads][head_dim] of `type` (any of the
  * three), rows q_stride values apart (at least n_q_heads * head_dim), aligned to its type; k likewise, with n_k_heads; either number of heads may be
- * 0 and its pointers null then.  q_out, k_out: of the same type and shape, the input itself (same stride) or not overlapping any input;
- * values between rows' ends and the next rows are left as they were.  inverse != 0: the angle's sign is turned (the transpose of the
+ * 0 and its pointers null then.  q_out, k_out: of the same type and shape, the input itself (same stride) or not overlapping anything that the call
+ * reads, nor each other (KV_ERR_ARG); values between rows' ends and the next rows are left as they were.  inverse != 0: the angle's sign is turned (the transpose of the
  * operation: it takes gradients back, and rows too, with a magnitude of 1).  Rows of 16-byte aligned heads are fastest.
  */
 int kv_rotary(const kv_rotary_t *rotary, const int32_t *positions, int64_t n_rows, int32_t type, int32_t inverse, const void *q,

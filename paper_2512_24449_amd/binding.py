@@ -810,7 +810,7 @@ class Rotary(_Operators):
     def kv_rotary(self, q, positions, k=None, out=None, k_out=None, inverse=False, stream=None):
         """q, k: fp16, bf16 or fp32 [rows, heads, head_dim] (or [batch, n, heads, head_dim]), both of one type; may be parts of wider rows.
         positions: int32, of q's shape without the last two axes.  Returns what became of q, or of (q, k); out and k_out: where to, which
-        may be q and k themselves.  inverse: turned the other way."""
+        may be q and k themselves, and else nothing that overlaps what is read.  inverse: turned the other way."""
         done = self._calls.turn(q, positions, k, out, k_out, inverse, stream)
         if done is not NotImplemented:
             return done

@@ -11,6 +11,7 @@
 #include <cmath>
 
 #include "common.h"
+#include "overlap.h"
 
 namespace packkv {
 
@@ -157,6 +158,17 @@ extern "C" int kv_rotary(const kv_rotary_t *rotary, const int32_t *positions, in
     r.splits = int(std::min<int64_t>(r.heads, std::max<int64_t>(ROTARY_SPLITS, ROTARY_SLOTS / n_rows)));
     const int64_t groups = (n_rows * r.splits + r.slots - 1) / r.slots;
     if (n_rows > (int64_t(1) << 40) || groups > (int64_t(1) << 24) - 1) return KV_ERR_UNSUPPORTED;
+    const auto rows = [&](const void *p, int64_t stride, int heads) {
+        return Rows(p, Rows::Wide(heads) * D * size, Rows::Wide(stride) * size, heads ? n_rows : 0);
+    };
+    const Rows in[2] = {rows(q, q_stride, n_q_heads), rows(k, k_stride, n_k_heads)};
+    const Rows out[2] = {rows(q_out, q_out_stride, n_q_heads), rows(k_out, k_out_stride, n_k_heads)};
+    for (int i = 0; i < 2; ++i) {
+        const bool own = both[i].in == both[i].out && (n_rows == 1 || both[i].in_stride == both[i].out_stride);
+        if ((!own && overlap(out[i], in[i])) || overlap(out[i], {in[1 - i], Rows(positions, n_rows, 4), Rows(rotary->turns, dims / 2, 8)}))
+            return KV_ERR_ARG;
+    }
+    if (overlap(out[0], out[1])) return KV_ERR_ARG;
     const bool streamed = n_rows * r.heads * int64_t(D) * int64_t(size) >= ROTARY_STREAMED;
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
     const bool i = rotary->interleaved != 0;
