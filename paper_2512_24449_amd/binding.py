@@ -729,6 +729,8 @@ class FP4KVCache(_Operators):
         shape, on = (batch.batch, self.n_kv_heads, keep), self._stream(stream)
         kept_at = self._plain(what, "kept", kept, torch.int32, shape)
         n_at = self._plain(what, "n_kept", n_kept, torch.int32, shape[:1])
+        if keep >= 2 ** 31:
+            _refuse(what, "kept has fewer than 2^31 positions to a head")
         if to.device != self.device or to.batch != batch.batch:
             _refuse(what, "both batches are on %s, of as many sequences" % self.device)
         if any(t is not None and t.dim() != 3 for t in (mass, mass_out)) or (mass is None and mass_out is not None):
@@ -834,7 +836,7 @@ class Rotary(_Operators):
             to_rows, to_pitch = self._row_pitch(what, to, heads, self.head_dim, (t.dtype,))
             if to.shape != t.shape:
                 _refuse(what, "an output is of its input's shape")
-            args += [t.data_ptr(), pitch, heads, to.data_ptr(), to_pitch]
+            args += [t.data_ptr(), pitch, min(heads, 65536), to.data_ptr(), to_pitch]     # (65535 at most: the library says so)
             made.append(to)
             kept += [t, to]
         self._made(what, _lib.kv_rotary, self._ref, positions.data_ptr(), positions.numel(), _TYPES[q.dtype], int(inverse), *args, stream)

@@ -479,7 +479,7 @@ bool turned_rows(const RotaryCalls *c, PyObject *o, c10::ScalarType type, Rows &
     if (!THPVariable_CheckExact(o)) return false;
     const at::Tensor &t = THPVariable_Unpack(o);
     if (t.layout() != c10::kStrided || t.scalar_type() != type || t.dim() != 3 || t.device() != c->device || t.size(2) != c->head_dim ||
-        t.stride(2) != 1 || (t.size(1) > 1 && t.stride(1) != c->head_dim) || t.is_conj() || t.is_neg())
+        t.size(1) > INT32_MAX || t.stride(2) != 1 || (t.size(1) > 1 && t.stride(1) != c->head_dim) || t.is_conj() || t.is_neg())
         return false;
     out = {&t, t.size(0), t.size(0) > 1 ? t.stride(0) : t.size(1) * c->head_dim};
     return true;
