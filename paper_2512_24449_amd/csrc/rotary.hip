@@ -155,9 +155,11 @@ extern "C" int kv_rotary(const kv_rotary_t *rotary, const int32_t *positions, in
              rotary->turns, D, dims, rotary->magnitude, inverse ? -1.0f : 1.0f, 0, 0, 0};
     r.units = (in_place ? dims : D) / (2 * width);
     r.slots = 256 / r.units;
-    r.splits = int(std::min<int64_t>(r.heads, std::max<int64_t>(ROTARY_SPLITS, ROTARY_SLOTS / n_rows)));
+    // A launch takes fewer than 2^32 threads: beyond, fewer slots to a row.
+    const int64_t slots = r.slots * ((int64_t(1) << 24) - 1);
+    if (n_rows > slots) return KV_ERR_UNSUPPORTED;
+    r.splits = int(std::min<int64_t>({r.heads, std::max<int64_t>(ROTARY_SPLITS, ROTARY_SLOTS / n_rows), slots / n_rows}));
     const int64_t groups = (n_rows * r.splits + r.slots - 1) / r.slots;
-    if (n_rows > (int64_t(1) << 40) || groups > (int64_t(1) << 24) - 1) return KV_ERR_UNSUPPORTED;
     const auto rows = [&](const void *p, int64_t stride, int heads) {
         return Rows(p, Rows::Wide(heads) * D * size, Rows::Wide(stride) * size, heads ? n_rows : 0);
     };
