@@ -100,20 +100,19 @@ __global__ __launch_bounds__(256) void rotary_kernel(Rotary r) {
 }
 
 // A row is spread over so many slots (if it has as many heads), and more in a call of few rows: sines are found anew in each, which
-// costs less than fewer threads do.  Outputs of 128 MB or more, half of the last-level cache, are stored past the caches.
-// 25077 bf16 rows of 40 heads (514 MB moved) with 8 / 20 / 40 slots to a row 98.7 / 93.9 / 93.8 us, so stored 94.0 / 89.4 / 89.2
-// (5.7 TB/s; a copy reaches 4.7 to 5.0).
+// costs less than fewer threads do.  25077 bf16 rows of 40 heads (514 MB moved) with 8 / 20 / 40 slots to a row 98.7 / 93.9 / 93.8 us.
+// Outputs of 128 MB or more, half of the last-level cache, are stored past the caches where pairs are halves apart: those rows 88.5 us
+// (5.8 TB/s; a copy reaches 4.7 to 5.0) for 93.2, fp32 178.5 for 184.7.  Interleaved pairs are stored by 16 bytes with as many between, which
+// the caches join: past them 120.7 us for 99.6, fp32 191.5 for 189.0.
 constexpr int64_t ROTARY_SPLITS = 20, ROTARY_SLOTS = 16384, ROTARY_STREAMED = int64_t(1) << 27;
 
 template <typename T, int V>
 int launch_rotary(const Rotary &r, bool interleaved, bool streamed, int64_t groups, hipStream_t s) {
     constexpr bool WIDE = sizeof(T) * V == 16;
 #define LAUNCH(I, S) hipLaunchKernelGGL((rotary_kernel<T, V, I, S>), dim3(uint32_t(groups)), dim3(256), 0, s, r)
-    if (WIDE && streamed) {
-        if (interleaved) LAUNCH(true, WIDE); else LAUNCH(false, WIDE);
-    } else {
-        if (interleaved) LAUNCH(true, false); else LAUNCH(false, false);
-    }
+    if (interleaved) LAUNCH(true, false);
+    else if (WIDE && streamed) LAUNCH(false, WIDE);
+    else LAUNCH(false, false);
 #undef LAUNCH
     KV_HIP_CHECK(hipGetLastError());
     return KV_OK;
