@@ -532,7 +532,8 @@ int kv_fp4_compact(kv_fp4_cache_t *cache, const kv_fp4_batch_t *from, const kv_f
  * `dims` channels of a head, channels (x, y) at (i, i + dims / 2), or (2i, 2i + 1) where interleaved, and a row's position p:
  *     a = 2 pi * p * turns[i] / 2^64
  *     x' = magnitude * (x cos a - y sin a),  y' = magnitude * (y cos a + x sin a)
- * Channels from dims on are copied.  Angles are exact to 2^-32 of a turn at any position, sums are fp32, rounded once.
+ * Channels from dims on are copied.  p * turns is exact modulo a turn and cut to 2^-32 of one, at any position; what it is more than a number of
+ * quarter turns then becomes an fp32 number of radians (off by 1.4e-7 at most).  Sums are fp32, rounded once.
  */
 typedef struct {
     int32_t head_dim;      /* even, 2 .. 512                                      */

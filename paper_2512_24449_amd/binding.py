@@ -755,7 +755,8 @@ class Rotary(_Operators):
                 blend that is linear in the turns
       "ramp"    f_i / factor of pairs that turn less than `slow` times, f_i of those that do more than `fast` times, in between a blend that is
                 linear in i; the turned channels are multiplied by 0.1 ln(factor) + 1
-    frequencies: all f_i, in radians, instead; magnitude: what the turned channels are multiplied by, instead.
+    frequencies: all f_i, in radians, instead; magnitude: what the turned channels are multiplied by, instead.  Frequencies are
+    doubles: an angle position * f_i is right to some 2^-52 of its size (5e-7 radians for f_i = 1 at the last of positions) before it is reduced.
 
     There is no backward pass; inverse=True is the transposed operation, which takes gradients back.  Streams as of FP4KVCache."""
 

@@ -7,11 +7,11 @@
 // 4g + i of a product is column 4i + g of the call's columns (row after row, the heads of the kv-head next to each other): with up
 // to four columns a lane has one exponential to a token, not four.
 //
-// Few columns are bound by HBM: 8 sequences x 52 heads x 32000 tokens, 1.01 GB, in 199 us, 5.1 TB/s (half of every block of a
+// Few columns are bound by HBM: 8 sequences x 52 heads x 32000 tokens, 1.01 GB, in 198 us, 5.1 TB/s (half of every block of a
 // page is read, and a tenth of the bytes is weights, read and written: a copy reaches 4.7 to 5.0, a read 5.9 to 6.8).  Many columns by
-// exponentials and products, which share the issue: 2048 rows of 32 heads at 12288 (2.2e11 operations) take 225 us, 990 TFLOP/s, where a
-// large library product reaches 1345; per 16 columns and page 68 vector instructions, 16 of them exponentials of four times the
-// cost, beside 16 products: vector instructions are issued 72 % of the time, the matrix cores are busy 40 %.
+// exponentials and products, which share the issue: 2048 rows of 32 heads at 12288 (2.2e11 operations) take 225 to 232 us by the card, 965 to
+// 990 TFLOP/s, where a large library product reaches 1345 (some 260 us in the first passes after a pause: the clock rises over
+// hundreds); per 16 columns and page 68 vector instructions, 16 of them exponentials of four times the cost, beside 16 products: vector instructions are issued 72 % of the time, the matrix cores are busy 40 %.
 #include "fp4_attention.h"
 #include "overlap.h"
 
@@ -434,9 +434,9 @@ __global__ __launch_bounds__(256) void fp4_weights_join_kernel(Fp4Weights a, int
 }
 
 // Pages of a wave: one to each of so many waves first (two workgroups to a compute unit).  With more columns than 16 no more
-// waves than these, so that each operand is fetched and laid out as seldom as may be; else up to so many pages.  With 1 / 2 / 4 / 8 / 16 pages to a
-// wave 8 x 52 heads x 32000 tokens take 281 / 219 / 203 / 202 / 206 us, four sequences of up to 32788 tokens, 8 kv-heads, 18.1 / 15.3 / 14.2 / 13.9 / 17 (12), 32 rows
-// of 32 heads at 131072 (128 columns) 53 / 47 / 45 / 41.7 / 53 (12).
+// waves than these, so that each operand is fetched and laid out as seldom as may be; else up to so many pages.  With 1 / 2 / 4 / 6 / 8 / 12 / 16
+// pages to a wave 8 x 52 heads x 32000 tokens take 281 / 217 / 200 / 198 / 199 / 202 / 204 us, four sequences of up to 32788 tokens, 8 kv-heads, 18.1 / 15.1 /
+// 14.0 / 14.7 / 13.8 / 17.1 / 17.0, 32 rows of 32 heads at 131072 (128 columns) 60 / 47 / 42 / 44 / 40 / 53 / 46.
 constexpr int64_t WEIGHTS_ROUND = 2048;
 constexpr int WEIGHTS_PAGES = 6;
 // Workgroups that many columns are split into; their sums are joined by a kernel.  The chunk of 2048 rows with 1 / 2 / 5 / 10 / 20 splits 299 / 292 / 238 /
