@@ -489,11 +489,11 @@ int kv_fp4_attention(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, const v
  * with q, sm_scale, window, sinks (and so which rows see t) and lse as the call of kv_fp4_attention on the same batch had or
  * gave them.  mass: device fp32 [batch][H_kv][mass_tokens]; written are the places of the tokens that the sequence holds
  * (and the page table and mass have room for), others are left as they were.  past: null (0), or of mass's
- * size, mass itself or not overlapping it (mass overlaps nothing else that the call reads: KV_ERR_ARG); it is not read for the call's own tokens, positions from lens - new_rows on, which
- * no earlier row has seen.  A token that no row sees, and one of a missing page, keeps past's.  max_new may be 0: mass is then past.
+ * size, mass itself or not overlapping it (mass overlaps nothing else that the call reads: KV_ERR_ARG); it is not read for the call's own
+ * tokens, positions from lens - new_rows on, which no earlier row has seen.  A token that no row sees, and one of a missing page, keeps past's.  max_new may be 0: mass is then past.
  * fp32 throughout, q.Khat as in attention; what lse is off by (a few 2^-24 of its size) is a factor of a row's weights.  A row whose lse is
- * -infinity gives nothing, whatever its q is; another whose q (unless sm_scale is 0) or lse is NaN makes the tokens that it sees NaN.  Sums have a fixed order: the result is bitwise
- * reproducible.  Uses the workspace: calls of kv_fp4_attention, kv_fp4_weights and kv_fp4_select on one cache must not overlap.
+ * -infinity gives nothing, whatever its q is; another whose q (unless sm_scale is 0) or lse is NaN makes the tokens that it sees NaN.  Sums
+ * have a fixed order: the result is bitwise reproducible.  Uses the workspace: calls of kv_fp4_attention, kv_fp4_weights and kv_fp4_select on one cache must not overlap.
  */
 int kv_fp4_weights(kv_fp4_cache_t *cache, const kv_fp4_batch_t *batch, const void *q, int64_t q_stride, int32_t type,
                    int64_t n_rows, float sm_scale, int32_t window, int32_t sinks, const float *lse, const float *past,
@@ -546,8 +546,8 @@ typedef struct {
  * positions: device int32 [n_rows], any values, read when the kernel runs.  q: device [n_rows][n_q_heads][head_dim] of `type` (any of the
  * three), rows q_stride values apart (at least n_q_heads * head_dim), aligned to its type; k likewise, with n_k_heads; either number of heads may be
  * 0 and its pointers null then.  q_out, k_out: of the same type and shape, the input itself (same stride) or not overlapping anything that the call
- * reads, nor each other (KV_ERR_ARG); values between rows' ends and the next rows are left as they were.  inverse != 0: the angle's sign is turned (the transpose of the
- * operation: it takes gradients back, and rows too, with a magnitude of 1).  Rows of 16-byte aligned heads are fastest.
+ * reads, nor each other (KV_ERR_ARG); values between rows' ends and the next rows are left as they were.  inverse != 0: the angle's sign is
+ * turned (the transpose of the operation: it takes gradients back, and rows too, with a magnitude of 1).  Rows of 16-byte aligned heads are fastest.
  */
 int kv_rotary(const kv_rotary_t *rotary, const int32_t *positions, int64_t n_rows, int32_t type, int32_t inverse, const void *q,
               int64_t q_stride, int32_t n_q_heads, void *q_out, int64_t q_out_stride, const void *k, int64_t k_stride,

@@ -9,9 +9,10 @@
 //
 // Few columns are bound by HBM: 8 sequences x 52 heads x 32000 tokens, 1.01 GB, in 198 us, 5.1 TB/s (half of every block of a
 // page is read, and a tenth of the bytes is weights, read and written: a copy reaches 4.7 to 5.0, a read 5.9 to 6.8).  Many columns by
-// exponentials and products, which share the issue: 2048 rows of 32 heads at 12288 (2.2e11 operations) take 225 to 232 us by the card, 965 to
+// exponentials and products, which share the issue: 2048 rows of 32 heads at 12288 (2.2e11 operations) take 225 to 237 us by the card, 945 to
 // 990 TFLOP/s, where a large library product reaches 1345 (some 260 us in the first passes after a pause: the clock rises over
-// hundreds); per 16 columns and page 68 vector instructions, 16 of them exponentials of four times the cost, beside 16 products: vector instructions are issued 72 % of the time, the matrix cores are busy 40 %.
+// hundreds); per 16 columns and page 68 vector instructions, 16 of them exponentials of four times the cost, beside 16 products: vector
+// instructions are issued 72 % of the time, the matrix cores are busy 40 %.
 #include "fp4_attention.h"
 #include "overlap.h"
 
